@@ -496,6 +496,49 @@ int octopus_attn_decode_paged_qjl(const octopus_codebooks_t *cb,
                                   void *workspace, size_t workspace_bytes,
                                   void *stream);
 
+/* ---- sequences that share a prefix (the pages of octopus_encode_paged / octopus_attn_decode_paged) ----
+ * A batch whose sequences all begin with the same tokens (a system prompt, the beams or samples of one prompt, drafts to be
+ * verified) holds those tokens once, in pages of their own, and each sequence's other tokens in that sequence's pages:
+ *   out = softmax(scale * q . k^_t) V over the prefix's tokens t < prefix_len[0] and the sequence's own ones,
+ * with the prefix's pages read once for the rows of all sequences (octopus_attn_decode_paged over a table that repeats them reads
+ * them once per sequence).  Where a token stands in its sequence is the caller's business (keys are rotated by position before they
+ * are encoded, if at all); the own tokens begin at slot 0 of the sequence's first page, whatever prefix_len is.
+ *   q            device, [n_seq][n_q][n_q_heads][d] contiguous, q_dtype F32/BF16, aligned to its element.  Query head h uses KV head
+ *                h / (n_q_heads / n_kv_heads).
+ *   q_lens       device int32 [n_seq] or NULL (all n_q): the queries of each sequence that count; a padded batch's others are not
+ *                looked at and their rows of out stay as they were.
+ *   causal       0: every query sees all own tokens; 1: query i of sequence s sees the prefix and its own tokens
+ *                t <= seq_lens[s] - q_lens[s] + i (the queries are those of the last q_lens[s] tokens; none where that is negative).
+ *   k_pool, v_pool, n_pages, signs   as for octopus_attn_decode_paged (bf16 values).
+ *   prefix_table device int32 [prefix_pages]: the page of the prefix's tokens 64 j .. 64 j + 63; ids clamped to the pool.
+ *   prefix_len   device int32 [1], 0 <= prefix_len <= max_prefix (clamped); max_prefix <= prefix_pages * 64, on the host, sizes the
+ *                launch.  max_prefix 0: no prefix; prefix_table and prefix_len are not looked at.
+ *   block_table, max_pages_per_seq, seq_lens, max_len   the own tokens, as for octopus_attn_decode_paged; max_len 0: none, and
+ *                block_table and seq_lens are not looked at.
+ *   out          device fp32 [n_seq][n_q][n_q_heads][d]; a query that sees no token yields zeros.
+ *   workspace    device, 256-byte aligned, at least octopus_attn_prefix_workspace(...) bytes of the same shape; contents are scratch.
+ * Values: a token that a query does not see for causality is a token of the sequence all the same, and one whose value is not a
+ * finite number makes outputs of its step's queries NaN; tokens past the lengths are never looked at.
+ * Any n_q, n_seq and head ratio (all n_seq * n_q * n_q_heads <= 2^26 rows, n_seq * n_q <= 2^24).  octopus_profile_events takes the call.
+ * Errors: EINVAL, EUNSUPPORTED (a plan or type without a kernel; the App. D pairs have none), EWORKSPACE, EHIP. */
+size_t octopus_attn_prefix_workspace(const octopus_codebooks_t *cb, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
+                                     int32_t n_q, int64_t max_prefix, int64_t max_len);
+
+int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb,
+                                     const void *q, int32_t q_dtype,
+                                     int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
+                                     const int32_t *q_lens, int32_t causal,
+                                     const uint8_t *signs,
+                                     const void *k_pool, const void *v_pool, int32_t n_pages,
+                                     const int32_t *prefix_table, int32_t prefix_pages,
+                                     const int32_t *prefix_len, int64_t max_prefix,
+                                     const int32_t *block_table, int32_t max_pages_per_seq,
+                                     const int32_t *seq_lens, int64_t max_len,
+                                     float scale,
+                                     float *out,
+                                     void *workspace, size_t workspace_bytes,
+                                     void *stream);
+
 /* Static, human-readable name of an error code. */
 const char *octopus_strerror(int code);
 

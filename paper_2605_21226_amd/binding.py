@@ -26,7 +26,8 @@ EXPORTS = ("octopus_build_codebooks", "octopus_build_codebooks_pair", "octopus_c
            "octopus_paged_pool_bytes", "octopus_encode_paged", "octopus_attn_decode_paged",
            "octopus_attn_decode_paged_hybrid", "octopus_encode_values_paged", "octopus_attn_decode_paged_vq",
            "octopus_encode_qjl_paged", "octopus_attn_decode_paged_qjl",
-           "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores")
+           "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores",
+           "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix")
 
 
 class Plan(ctypes.Structure):
@@ -135,6 +136,11 @@ def load():
     lib.octopus_attn_decode_paged_qjl.argtypes = [CB, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, i32, vp,
                                                   i64, f32, vp, vp, ctypes.c_size_t, vp]
     lib.octopus_attn_decode_paged_qjl.restype = ctypes.c_int
+    lib.octopus_attn_prefix_workspace.argtypes = [CB, i32, i32, i32, i32, i64, i64]
+    lib.octopus_attn_prefix_workspace.restype = ctypes.c_size_t
+    lib.octopus_attn_decode_paged_prefix.argtypes = [CB, vp, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, i32, vp, i32, vp, i64, vp,
+                                                     i32, vp, i64, f32, vp, vp, ctypes.c_size_t, vp]
+    lib.octopus_attn_decode_paged_prefix.restype = ctypes.c_int
     lib.octopus_vq_on_matrix_cores.argtypes = [ctypes.POINTER(Codebooks), i32, i32, i32, i32, i32]
     lib.octopus_vq_on_matrix_cores.restype = ctypes.c_int
     lib.octopus_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
@@ -468,6 +474,32 @@ def octopus_attn_decode_paged_qjl(cb, q, signs, signs2, k_pool, qjl_pool, v_pool
                                                 _ptr(seq_lens), int(max_len), float(scale), _ptr(out), _ptr(workspace),
                                                 int(workspace.numel() * workspace.element_size()), _stream_ptr(stream))
     _check(code, "octopus_attn_decode_paged_qjl")
+
+
+def octopus_attn_prefix_workspace(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len):
+    return int(load().octopus_attn_prefix_workspace(ctypes.byref(cb), int(n_seq), int(n_q_heads), int(n_kv_heads), int(n_q),
+                                                    int(max_prefix), int(max_len)))
+
+
+def octopus_attn_decode_paged_prefix(cb, q, signs, k_pool, v_pool, prefix_table, prefix_len, max_prefix, block_table, seq_lens,
+                                     max_len, scale, out, workspace, q_lens=None, causal=False, stream=None):
+    """Attention of sequences that share a prefix: q device [n_seq, n_q, n_q_heads, d] contiguous, v_pool device bf16 [n_pages,
+    n_kv_heads, 64, d] contiguous, prefix_table device int32 [prefix_pages], prefix_len device int32 [1], block_table device int32
+    [n_seq, max_pages_per_seq] and seq_lens device int32 [n_seq] of the own tokens (None, None with max_len 0, as prefix_table and
+    prefix_len with max_prefix 0), q_lens device int32 [n_seq] or None."""
+    assert q.is_contiguous() and v_pool.is_contiguous() and out.is_contiguous()
+    n_seq, n_q, n_qh, d = q.shape
+    n_pages, n_kv = v_pool.shape[0], v_pool.shape[1]
+    assert tuple(v_pool.shape[2:]) == (64, d) and _dtype_code(v_pool) == DTYPE_BF16
+    assert out.shape == q.shape and _dtype_code(out) == DTYPE_F32
+    assert prefix_table is None or prefix_table.is_contiguous()
+    assert block_table is None or (block_table.is_contiguous() and block_table.shape[0] == n_seq)
+    code = load().octopus_attn_decode_paged_prefix(
+        ctypes.byref(cb), _ptr(q), _dtype_code(q), n_seq, n_qh, n_kv, n_q, _ptr(q_lens), int(bool(causal)), _ptr(signs), _ptr(k_pool),
+        _ptr(v_pool), n_pages, _ptr(prefix_table), 0 if prefix_table is None else prefix_table.numel(), _ptr(prefix_len),
+        int(max_prefix), _ptr(block_table), 0 if block_table is None else block_table.shape[1], _ptr(seq_lens), int(max_len),
+        float(scale), _ptr(out), _ptr(workspace), int(workspace.numel() * workspace.element_size()), _stream_ptr(stream))
+    _check(code, "octopus_attn_decode_paged_prefix")
 
 
 def octopus_profile_events(before, after):

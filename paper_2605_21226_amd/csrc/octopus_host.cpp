@@ -220,6 +220,8 @@ bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 
 }  // namespace
 
+bool plan_well_formed(const octopus_plan_t &plan) { return plan_consistent(plan); }
+
 DecodeShape make_decode_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
                               int32_t n_q, int64_t max_len, int64_t t_capacity, bool many_rows, int32_t rows_cap,
                               int32_t vq_mfma_waves, int32_t rows_min, bool wide_rows) {
@@ -351,6 +353,12 @@ thread_local void *g_event_before = nullptr;
 thread_local void *g_event_after = nullptr;
 }  // namespace
 
+void octopus::take_profile_events(void **before, void **after) {
+    *before = g_event_before;
+    *after = g_event_after;
+    g_event_before = g_event_after = nullptr;
+}
+
 extern "C" {
 
 int octopus_profile_events(void *before, void *after) {
@@ -443,6 +451,12 @@ static bool seed_grid_ok(const octopus_codebooks_t &cb) {
     }
     return true;
 }
+
+}  // extern "C"
+
+bool octopus::encoder_takes(const octopus_codebooks_t &cb) { return seed_grid_ok(cb); }
+
+extern "C" {
 
 static int encode_checked(const octopus_codebooks_t *cb, const void *keys, int32_t key_dtype, int64_t stride_seq,
                           int64_t stride_tok, int64_t stride_head, int32_t n_seq, int32_t n_kv_heads, int32_t n_new,

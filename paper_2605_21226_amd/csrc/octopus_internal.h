@@ -152,6 +152,34 @@ int launch_decode_vq(const octopus_codebooks_t &cb, const DecodeShape &s, const 
                      float *part_acc, float *scores_out, int32_t *work_plan, void *stream,
                      PageTable pt = PageTable{nullptr, 0, 0});   // pt: cache and vq are pools of pages
 
+// Attention of sequences that share a prefix (octopus_prefix.hpp).  A segment is one workgroup's share: a range of the prefix's or of a
+// sequence's tokens for 32 query rows of one KV head; the prefix's segments come first.
+struct PrefixShape {
+    int32_t n_seq, n_q_heads, n_kv_heads, n_q;
+    int32_t max_prefix, max_len, max_pages, n_pages;
+    int32_t causal, q_is_bf16;
+    const void *q;
+    const uint8_t *signs;
+    float scale;
+    int32_t prefix_groups, prefix_splits, own_groups, own_splits;   // groups of 32 rows, ranges of tokens
+    int32_t prefix_segments, n_segments;
+    int64_t own_partials;   // partial results before the first of a sequence's own (one per query row and range)
+};
+// The division of a call (n_segments 0: no tokens at all) and how many partial results it has at most.
+PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
+                              int64_t max_prefix, int64_t max_len, int64_t *partials);
+int launch_prefix(const octopus_codebooks_t &cb, const PrefixShape &s, const void *k_pool, const void *v_pool, const int32_t *prefix_table,
+                  const int32_t *prefix_len, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens, float *part_ml,
+                  float *part_acc, void *stream);
+int launch_prefix_merge(const octopus_plan_t &plan, const PrefixShape &s, const int32_t *prefix_len, const int32_t *seq_lens,
+                        const int32_t *q_lens, const float *part_ml, const float *part_acc, float *out, void *stream);
+
+// What the entry points outside octopus_host.cpp ask of it: a plan whose parts fit together, codebooks the encoder takes, and the
+// measurement events armed for this thread's next decode-attention call (forgotten by the asking).
+bool plan_well_formed(const octopus_plan_t &plan);
+bool encoder_takes(const octopus_codebooks_t &cb);
+void take_profile_events(void **before, void **after);
+
 // Measurement aid: plain streaming read of `bytes` bytes by n_blocks workgroups (non-temporal loads or not).
 int launch_probe_read(const void *data, int64_t bytes, int nontemporal, int n_blocks, void *sink, void *stream);
 

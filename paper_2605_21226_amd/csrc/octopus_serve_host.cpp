@@ -1,0 +1,129 @@
+// Host side of the entry points over pages that a server calls around the attention: checks of arguments, division of the work,
+// launches.
+#include <algorithm>
+#include <cmath>
+
+#include "octopus_internal.h"
+
+namespace octopus {
+namespace {
+
+bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+bool pages_ok(const void *table, int32_t pages) {
+    return table != nullptr && aligned(table, 4) && pages >= 1 && pages <= INT32_MAX / OCTOPUS_TILE;
+}
+
+int prefix_args(const octopus_codebooks_t *cb, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q, int64_t max_prefix,
+                int64_t max_len) {
+    if (cb == nullptr) return OCTOPUS_EINVAL;
+    if (n_seq < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q < 1 || n_q_heads % n_kv_heads != 0) return OCTOPUS_EINVAL;
+    if (max_prefix < 0 || max_prefix > INT32_MAX - OCTOPUS_TILE || max_len < 0 || max_len > INT32_MAX - OCTOPUS_TILE) return OCTOPUS_EINVAL;
+    // rows, segments and threads of a launch are counted in 32 bits
+    if (static_cast<int64_t>(n_seq) * n_q > (1 << 24) || static_cast<int64_t>(n_seq) * n_q * n_q_heads > (1 << 26)) return OCTOPUS_EINVAL;
+    if (!plan_well_formed(cb->plan)) return OCTOPUS_EINVAL;
+    if (!plan_supported(cb->plan)) return OCTOPUS_EUNSUPPORTED;
+    return OCTOPUS_OK;
+}
+
+}  // namespace
+
+// Ranges of tokens: a workgroup's segment takes rounds of one step per wavefront and a start of its own (queries, results), the
+// workgroups run in rounds of 256, and every range writes a partial result per query row that the merge reads again.  The number of
+// rounds a segment has at most is the one that makes the least of all that.
+PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
+                              int64_t max_prefix, int64_t max_len, int64_t *partials) {
+    PrefixShape s{};
+    s.n_seq = n_seq;
+    s.n_q_heads = n_q_heads;
+    s.n_kv_heads = n_kv_heads;
+    s.n_q = n_q;
+    s.max_prefix = static_cast<int32_t>(max_prefix);
+    s.max_len = static_cast<int32_t>(max_len);
+    const int64_t hpk = n_q_heads / n_kv_heads, own_rows = n_q * hpk, all_rows = own_rows * n_seq;
+    s.prefix_groups = static_cast<int32_t>((all_rows + 31) / 32);
+    s.own_groups = static_cast<int32_t>((own_rows + 31) / 32);
+    const int64_t round_keys = 32 * (plan.head_dim <= 128 ? 8 : 4);
+    const int64_t prefix_rounds = (max_prefix + round_keys - 1) / round_keys, own_rounds = (max_len + round_keys - 1) / round_keys;
+    const int64_t prefix_units = static_cast<int64_t>(n_kv_heads) * s.prefix_groups, own_units = static_cast<int64_t>(n_seq) * n_kv_heads * s.own_groups;
+    auto ranges = [](int64_t rounds, int64_t most) { return rounds == 0 ? 0 : std::min<int64_t>((rounds + most - 1) / most, 128); };
+    double best = INFINITY;
+    for (int64_t most = 1; most <= std::max<int64_t>(1, std::max(prefix_rounds, own_rounds)); most += std::max<int64_t>(1, most / 16)) {
+        const int64_t a = ranges(prefix_rounds, most), b = ranges(own_rounds, most);
+        const int64_t segments = prefix_units * a + own_units * b;
+        if (segments > INT32_MAX / 2 && most < std::max(prefix_rounds, own_rounds)) continue;
+        const double cost = static_cast<double>((segments + 255) / 256) * (2.5 + most) + static_cast<double>(all_rows) * n_kv_heads * (a + b) * 2e-5;
+        if (cost < best) {
+            best = cost;
+            s.prefix_splits = static_cast<int32_t>(a);
+            s.own_splits = static_cast<int32_t>(b);
+            s.prefix_segments = static_cast<int32_t>(prefix_units * a);
+            s.n_segments = static_cast<int32_t>(segments);
+        }
+    }
+    s.own_partials = all_rows * n_kv_heads * s.prefix_splits;
+    *partials = all_rows * n_kv_heads * (static_cast<int64_t>(s.prefix_splits) + s.own_splits);
+    return s;
+}
+
+}  // namespace octopus
+
+using namespace octopus;
+
+extern "C" {
+
+size_t octopus_attn_prefix_workspace(const octopus_codebooks_t *cb, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
+                                     int64_t max_prefix, int64_t max_len) {
+    if (prefix_args(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len) != OCTOPUS_OK) return 0;
+    int64_t partials = 0;
+    make_prefix_shape(cb->plan, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len, &partials);
+    return 256 + up256(partials * 2 * sizeof(float)) + up256(partials * static_cast<size_t>(cb->plan.head_dim) * sizeof(float));
+}
+
+int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb, const void *q, int32_t q_dtype, int32_t n_seq, int32_t n_q_heads,
+                                     int32_t n_kv_heads, int32_t n_q, const int32_t *q_lens, int32_t causal, const uint8_t *signs,
+                                     const void *k_pool, const void *v_pool, int32_t n_pages, const int32_t *prefix_table,
+                                     int32_t prefix_pages, const int32_t *prefix_len, int64_t max_prefix, const int32_t *block_table,
+                                     int32_t max_pages_per_seq, const int32_t *seq_lens, int64_t max_len, float scale, float *out,
+                                     void *workspace, size_t workspace_bytes, void *stream) {
+    void *before = nullptr, *after = nullptr;
+    take_profile_events(&before, &after);
+    const int ok = prefix_args(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len);
+    if (ok != OCTOPUS_OK) return ok;
+    if (q == nullptr || signs == nullptr || k_pool == nullptr || v_pool == nullptr || out == nullptr || n_pages < 1) return OCTOPUS_EINVAL;
+    if (causal != 0 && causal != 1) return OCTOPUS_EINVAL;
+    if (max_prefix > 0) {
+        if (!pages_ok(prefix_table, prefix_pages) || prefix_len == nullptr || !aligned(prefix_len, 4)) return OCTOPUS_EINVAL;
+        if (max_prefix > static_cast<int64_t>(prefix_pages) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
+    }
+    if (max_len > 0) {
+        if (!pages_ok(block_table, max_pages_per_seq) || seq_lens == nullptr || !aligned(seq_lens, 4)) return OCTOPUS_EINVAL;
+        if (max_len > static_cast<int64_t>(max_pages_per_seq) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
+    }
+    if (q_dtype != OCTOPUS_DTYPE_F32 && q_dtype != OCTOPUS_DTYPE_BF16) return OCTOPUS_EUNSUPPORTED;
+    if (!aligned(q, q_dtype == OCTOPUS_DTYPE_F32 ? 4 : 2) || !aligned(out, 4) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
+        !aligned(q_lens, 4) || !std::isfinite(scale))
+        return OCTOPUS_EINVAL;
+    const size_t need = octopus_attn_prefix_workspace(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len);
+    if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need) return OCTOPUS_EWORKSPACE;
+    int64_t partials = 0;
+    PrefixShape s = make_prefix_shape(cb->plan, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len, &partials);
+    s.max_pages = max_pages_per_seq;
+    s.n_pages = n_pages;
+    s.causal = causal;
+    s.q = q;
+    s.q_is_bf16 = q_dtype == OCTOPUS_DTYPE_BF16 ? 1 : 0;
+    s.signs = signs;
+    s.scale = scale;
+    float *part_ml = static_cast<float *>(workspace);
+    float *part_acc = reinterpret_cast<float *>(static_cast<char *>(workspace) + up256(partials * 2 * sizeof(float)));
+    int err = before != nullptr ? record_event(before, stream) : 0;
+    if (err == 0 && s.n_segments > 0)
+        err = launch_prefix(*cb, s, k_pool, v_pool, prefix_table, prefix_len, block_table, seq_lens, q_lens, part_ml, part_acc, stream);
+    if (err == 0 && after != nullptr) err = record_event(after, stream);
+    if (err == 0) err = launch_prefix_merge(cb->plan, s, prefix_len, seq_lens, q_lens, part_ml, part_acc, out, stream);
+    return err == 0 ? OCTOPUS_OK : OCTOPUS_EHIP;
+}
+
+}  // extern "C"
