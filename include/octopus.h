@@ -503,7 +503,7 @@ int octopus_attn_decode_paged_qjl(const octopus_codebooks_t *cb,
  * with the prefix's pages read once for the rows of all sequences (octopus_attn_decode_paged over a table that repeats them reads
  * them once per sequence).  Where a token stands in its sequence is the caller's business (keys are rotated by position before they
  * are encoded, if at all); the own tokens begin at slot 0 of the sequence's first page, whatever prefix_len is.
- *   q            device, [n_seq][n_q][n_q_heads][d] contiguous, q_dtype F32/BF16, aligned to its element.  Query head h uses KV head
+ *   q            device, [n_seq][n_q][n_q_heads][d] contiguous, q_dtype F32/BF16, 4-byte aligned.  Query head h uses KV head
  *                h / (n_q_heads / n_kv_heads).
  *   q_lens       device int32 [n_seq] or NULL (all n_q): the queries of each sequence that count; a padded batch's others are not
  *                looked at and their rows of out stay as they were.

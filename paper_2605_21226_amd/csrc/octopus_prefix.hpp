@@ -25,13 +25,16 @@ typedef uint32_t prefix_u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kPrefixKeys = 32;      // tokens of a step
-constexpr int kPrefixRows = 32;      // query rows of a wavefront: two blocks of 16
 constexpr float kUnitScale = 256.0f; // the table's numbers are 256 rho n: the remainders of small ones stay above fp16's denormals
 
 template <class P>
 struct PrefixCfg {
     static constexpr int D = P::D;
-    static constexpr int NW = D <= 128 ? 8 : 4;                    // wavefronts of a workgroup: what LDS and registers hold
+    // Wavefronts of a workgroup (two per SIMD, or one with all its registers) and blocks of 16 query rows of each: a key is decoded
+    // once for a wavefront's rows.
+    static constexpr int NW = D <= 128 ? 8 : 4;
+    static constexpr int RB = 2;
+    static constexpr int ROWS = 16 * RB;
     static constexpr int NT = kWave * NW;
     // triplets of each class that a lane group decodes; one class: padded to whole operands
     static constexpr int T0 = P::NCLASS == 1 ? ((P::NTRI + 7) / 8) * 2 : (P::NT0 + 3) / 4;
@@ -47,14 +50,22 @@ struct PrefixCfg {
     static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : 65536);
     static constexpr int R1 = P::NCLASS == 2 ? rep(E1 * 16, 16384) : 1;
     static constexpr int log2i(int x) { return x <= 1 ? 0 : 1 + log2i(x / 2); }
-    static constexpr int REC = P::GRANULES * kPrefixKeys * 16;     // bytes of a step's records
-    static constexpr int VST = 2 * D + 32;                         // bytes of a staged value row: four rows lie on 32 different banks
-    static constexpr int STAGE = REC + kPrefixKeys * VST;          // bytes of a wavefront's staging area
-    static constexpr int NREC = (REC + 1023) / 1024;               // 16-byte pieces per lane
+    static constexpr int RST = (P::GRANULES + 1) * 16;             // bytes of a staged record: keys that follow each other on other banks
+    static constexpr int REC = RST * kPrefixKeys;                  // bytes of a step's records
+    static constexpr int NREC = (P::GRANULES + 1) / 2;              // 16-byte pieces per lane
+    // A step's value rows go from memory to LDS directly, 1 KB per instruction: instruction i takes rows i, i + NVAL, ..; 32 bytes
+    // between the instructions' pieces put four rows that follow each other on 32 different banks (the transposed reads take four).
     static constexpr int NVAL = D / 16;
-    static constexpr int QOP = kPrefixRows * 4 * KS * 16;          // bytes of the query operands, leading parts (the remainders as many)
-    static_assert(2 * QOP <= NW * STAGE, "the query operands share the staging areas");
-    static_assert(NW * 16 * D * 4 <= NW * STAGE + 0 * D, "so do the wavefronts' results");
+    static constexpr int VST = 1024 + 32;
+    static constexpr int VAL = NVAL * VST;                         // bytes of a step's values
+    // Query operands in LDS: a row's leading parts and its remainders; rows 16 bytes apart beyond their size, so that the 16 rows read
+    // at once lie on all banks.  The wavefronts' results: rows 16 bytes apart for the same reason.  Both take the values' place.
+    static constexpr int QST = 2 * 4 * KS * 16 + 16;
+    static constexpr int OST = D + 4;                              // floats
+    static constexpr int PLACE = (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL) > NW * 16 * OST * 4 ? (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL)
+                                                                                               : NW * 16 * OST * 4;
+    // The transform of the queries: eight coordinates a thread.
+    static constexpr int QLANES = D / 8, QROWS = NT / QLANES, QPASS = (ROWS + QROWS - 1) / QROWS;
 };
 
 template <class P>
@@ -62,9 +73,9 @@ struct PrefixSmem {
     using C = PrefixCfg<P>;
     uint4 tab0[C::E0 * C::R0];
     uint4 tab1[P::NCLASS == 2 ? C::E1 * C::R1 : 1];
-    unsigned char stage[C::NW][C::STAGE];
-    float ml[C::NW][kPrefixRows][2];
-    float factor[kPrefixRows];         // of a row's scores
+    unsigned char rec[C::NW][C::REC];
+    float ml[C::NW][C::ROWS][2];
+    float factor[C::ROWS];         // of a row's scores
     float c_xi[P::NCLASS][1 << (P::BD0 > P::BD1 ? P::BD0 : P::BD1)];
     float c_rho[P::NCLASS][1 << (P::BN0 > P::BN1 ? P::BN0 : P::BN1)];
 };
@@ -82,6 +93,25 @@ __device__ __forceinline__ uint4 half_triplet(float x, float y, float z) {
     r.z = two(x - lower(r.x), y - lower(r.x >> 16));
     r.w = two(z - lower(r.y), 0.0f);
     return r;
+}
+
+// Two fp32 numbers as bf16, rounded to the nearest, the first in the lower half.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+
+// Until at most N of the loads from memory asked for are on their way (they arrive in order), and until LDS has answered.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+    __asm__ volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    __asm__ volatile("" ::: "memory");
 }
 
 template <class P>
@@ -122,16 +152,17 @@ struct QuarterStream {
 };
 
 template <class P>
-__global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_eu(PrefixCfg<P>::D <= 128 ? 2 : 1))) void prefix_attention_kernel(
+__global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_eu(PrefixCfg<P>::NW / 4))) void prefix_attention_kernel(
     DeviceBooks books, PrefixShape shp, const unsigned char *__restrict__ k_pool, const unsigned char *__restrict__ v_pool,
     const int32_t *__restrict__ prefix_table, const int32_t *__restrict__ prefix_len, const int32_t *__restrict__ block_table,
     const int32_t *__restrict__ seq_lens, const int32_t *__restrict__ q_lens, float *__restrict__ part_ml,
     float *__restrict__ part_acc) {
     using C = PrefixCfg<P>;
-    constexpr int D = P::D, NW = C::NW, KS = C::KS;
+    constexpr int D = P::D, NW = C::NW, KS = C::KS, RB = C::RB;
     constexpr int CB = D / 16;                       // blocks of 16 channels
     constexpr int64_t TILEB = P::GRANULES * kWave * 16, VTILEB = static_cast<int64_t>(kWave) * D * 2;
     __shared__ __attribute__((aligned(16))) PrefixSmem<P> sm;
+    __shared__ __attribute__((aligned(16))) unsigned char place[C::PLACE];   // (an object of its own: reads of the tables need not wait for it)
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, g = lane >> 4;
@@ -150,23 +181,20 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     __syncthreads();
     build_prefix_tables<P>(sm, tid);
 
-    unsigned char *stage = sm.stage[wave];
-    // where this lane's code words lie in the staged records (of key n; + 256 for key 16 + n)
+    unsigned char *stage = sm.rec[wave], *vals = place + wave * C::VAL;
     constexpr int DQ0 = C::T0 * 2 * P::BD0, NQ0 = C::T0 * P::BN0, DQ1 = C::T1 * 2 * P::BD1, NQ1 = C::T1 * P::BN1;
     using SD0 = QuarterStream<P::DIR0_BIT, DQ0>;
     using SN0 = QuarterStream<P::NRM0_BIT, NQ0>;
     using SD1 = QuarterStream<P::DIR1_BIT, (DQ1 > 0 ? DQ1 : 32)>;
     using SN1 = QuarterStream<P::NRM1_BIT, (NQ1 > 0 ? NQ1 : 32)>;
-    auto word_at = [&](int w) { return ((w >> 2) * (kPrefixKeys * 16)) + (w & 3) * 4 + n * 16; };
-    // (the last quarter's padding may lie past the record: words past it are its last one, and their terms meet zeros)
+    // (the last quarter's padding may lie past the record, in the 16 bytes between two records or in the next: its terms meet zeros)
     auto quarter = [&](auto stream_, int start, int quarter_bits, auto &words, int block) __attribute__((always_inline)) {
         using S = decltype(stream_);
         const int bit = start + g * quarter_bits;
-        const int first = bit >> 5;
+        const unsigned char *first = stage + n * C::RST + (bit >> 5) * 4 + block * (16 * C::RST);
         uint32_t raw[S::READ];
 #pragma unroll
-        for (int j = 0; j < S::READ; ++j)
-            raw[j] = *reinterpret_cast<const uint32_t *>(stage + word_at(min(first + j, P::NWORDS - 1)) + block * 256);
+        for (int j = 0; j < S::READ; ++j) raw[j] = *reinterpret_cast<const uint32_t *>(first + 4 * j);
         if constexpr (S::ALIGNED) {
 #pragma unroll
             for (int j = 0; j < S::WORDS; ++j) words[j] = raw[j];
@@ -179,7 +207,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     const int hpk = shp.n_q_heads / shp.n_kv_heads;
     const int all_rows = shp.n_seq * shp.n_q * hpk, own_rows = shp.n_q * hpk;
     // what a factor of 256 in the keys and the units of log2 make of the caller's scale
-    const float norm = shp.scale * kLog2e * (D == 64 ? 0.125f : (D == 128 ? 0.08838834764831845f : 0.0625f)) / kUnitScale;
+    // (its sign is the queries': a row's factor is not negative, so the largest product is the largest score's)
+    const float norm = fabsf(shp.scale) * kLog2e * (D == 64 ? 0.125f : (D == 128 ? 0.08838834764831845f : 0.0625f)) / kUnitScale;
 
     for (int seg = blockIdx.x; seg < shp.n_segments; seg += gridDim.x) {
         // ---- which (prefix or sequence, KV head, row group, split) this is ----
@@ -196,169 +225,185 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         const int begin = split * per, end = min(begin + per, steps);
         if (begin >= end) continue;   // (nothing of it is written and the merge reads nothing of it; uniform over the workgroup)
         const int32_t *pages = shared ? prefix_table : block_table + static_cast<int64_t>(seq) * shp.max_pages;
-        const int rows = shared ? all_rows : own_rows, row0 = grp * kPrefixRows;
-        const int live = min(2, (rows - row0 + 15) / 16);               // blocks of 16 rows with rows
+        const int rows = shared ? all_rows : own_rows, row0 = grp * C::ROWS;
+        const int live = min(RB, (rows - row0 + 15) / 16);              // blocks of 16 rows with rows
 
-        // ---- a step's records and values: from memory to registers ----
-        prefix_u32x4_t rec[C::NREC], val[C::NVAL];
+        // ---- a step's records, from memory to registers and from there to LDS; its values, from memory to LDS ----
+        prefix_u32x4_t rec[C::NREC];
+        // the pages of the wavefront's next 64 steps, one a lane
+        int held = 0, held_from = 0;
+        auto hold_pages = [&](int step) __attribute__((always_inline)) {
+            held_from = step;
+            held = pages[min(step + lane * NW, end - 1) / 2];
+        };
         auto page_of = [&](int step) __attribute__((always_inline)) {
-            return min(max(pages[min(step, end - 1) / 2], 0), shp.n_pages - 1);
+            return min(max(__builtin_amdgcn_readlane(held, (step - held_from) / NW), 0), shp.n_pages - 1);
         };
-        auto load_step = [&](int step, int page) __attribute__((always_inline)) {
-            const int64_t tile = static_cast<int64_t>(page) * shp.n_kv_heads + kvh;
-            const int first = (step & 1) * kPrefixKeys;   // of the page's tokens
-            const unsigned char *src = k_pool + tile * TILEB + first * 16;
-#pragma unroll
-            for (int e = 0; e < C::NREC; ++e) {
-                const int piece = min(lane + 64 * e, P::GRANULES * kPrefixKeys - 1);
-                rec[e] = *reinterpret_cast<const prefix_u32x4_t *>(src + (piece / kPrefixKeys) * (kWave * 16) + (piece % kPrefixKeys) * 16);
-            }
-            // (value rows past the end are the last one: their probabilities are zero, but what lies there may be no number)
-            const unsigned char *vsrc = v_pool + tile * VTILEB;
-            const int last = len - 1 - step * kPrefixKeys;
-#pragma unroll
-            for (int e = 0; e < C::NVAL; ++e) {
-                const int piece = lane + 64 * e, row = first + min(piece / (D / 8), last);
-                val[e] = *reinterpret_cast<const prefix_u32x4_t *>(vsrc + row * (2 * D) + (piece % (D / 8)) * 16);
-            }
-        };
-        auto store_step = [&]() __attribute__((always_inline)) {
+        constexpr bool HALF = P::GRANULES % 2 != 0;       // (an odd number of granules: the last piece is half the lanes')
+        const int rec_at = (lane / kPrefixKeys) * (kWave * 16) + (lane % kPrefixKeys) * 16;
+        auto load_records = [&](int step, int page) __attribute__((always_inline)) {
+            const unsigned char *src = k_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * TILEB + (step & 1) * (kPrefixKeys * 16);
 #pragma unroll
             for (int e = 0; e < C::NREC; ++e)
-                if (C::REC % 1024 == 0 || lane + 64 * e < P::GRANULES * kPrefixKeys)
-                    *reinterpret_cast<prefix_u32x4_t *>(stage + (lane + 64 * e) * 16) = rec[e];
+                if (!HALF || e + 1 < C::NREC || lane < 32)
+                    rec[e] = *reinterpret_cast<const prefix_u32x4_t *>(src + e * (2 * kWave * 16) + rec_at);
+        };
+        auto store_records = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < C::NVAL; ++e) {
-                const int piece = lane + 64 * e;
-                *reinterpret_cast<prefix_u32x4_t *>(stage + C::REC + (piece / (D / 8)) * C::VST + (piece % (D / 8)) * 16) = val[e];
-            }
+            for (int e = 0; e < C::NREC; ++e)
+                if (!HALF || e + 1 < C::NREC || lane < 32)
+                    *reinterpret_cast<prefix_u32x4_t *>(stage + (lane % kPrefixKeys) * C::RST + (lane / kPrefixKeys + 2 * e) * 16) = rec[e];
+        };
+        constexpr int LPR = D / 8;                       // lanes per value row
+        const int val_at = (lane / LPR) * (C::NVAL * 2 * D) + (lane % LPR) * 16;
+        auto load_values = [&](int step, int page) __attribute__((always_inline)) {
+            const unsigned char *src = v_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * VTILEB + (step & 1) * (kPrefixKeys * 2 * D) + val_at;
+#pragma unroll
+            for (int e = 0; e < C::NVAL; ++e)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + e * (2 * D)),
+                                                 (__attribute__((address_space(3))) void *)(vals + e * C::VST), 16, 0, 0);
         };
         const bool work = begin + wave < end;
-        int next_page = 0;
         if (work) {
-            load_step(begin + wave, page_of(begin + wave));
-            next_page = page_of(begin + wave + NW);
+            hold_pages(begin + wave);
+            load_records(begin + wave, page_of(begin + wave));
         }
 
-        // ---- the segment's queries: rotated, then as operands through LDS ----
+        // ---- the segment's queries: asked for before the tables are complete, rotated, then as operands through LDS ----
+        const int qc = tid % C::QLANES;                  // coordinates 8 qc .. + 7
+        prefix_u32x4_t asked[C::QPASS][2];
+        const uint32_t sbits = shp.signs[kvh * (D / 8) + qc];
+#pragma unroll
+        for (int p = 0; p < C::QPASS; ++p) {
+            typedef uint32_t u32x4a_t __attribute__((ext_vector_type(4), aligned(4)));
+            const int row = min(row0 + tid / C::QLANES + p * C::QROWS, rows - 1);
+            const int64_t at = ((static_cast<int64_t>(seq) * shp.n_q + row / hpk) * shp.n_q_heads + kvh * hpk + row % hpk) * D + 8 * qc;
+            const unsigned char *src = static_cast<const unsigned char *>(shp.q) + at * (shp.q_is_bf16 ? 2 : 4);
+            asked[p][0] = *reinterpret_cast<const u32x4a_t *>(src);
+            asked[p][1] = *reinterpret_cast<const u32x4a_t *>(src + (shp.q_is_bf16 ? 0 : 16));
+        }
         __syncthreads();                 // tables complete; the last segment's results have been read
-        unsigned char *qop = sm.stage[0];
-        for (int e = tid; e < 2 * C::QOP / 16; e += C::NT) reinterpret_cast<uint4 *>(qop)[e] = make_uint4(0u, 0u, 0u, 0u);
-        __syncthreads();
-        {
-            constexpr int EPL = D / 64, RPW = kPrefixRows / NW;
-            int slot[EPL];
 #pragma unroll
-            for (int j = 0; j < EPL; ++j) {
-                const int c = lane + 64 * j, t = c / 3;
-                const bool second = P::NCLASS == 2 && t >= P::NT0;
-                const int of = second ? t - P::NT0 : t, each = second ? (C::T1 > 0 ? C::T1 : 1) : C::T0;
-                const int at = of % each + (second ? C::T0 : 0);
-                slot[j] = ((of / each) * KS + at / 2) * 16 + ((at % 2) * 4 + c % 3) * 2;
+        for (int p = 0; p < C::QPASS; ++p) {
+            const int local = tid / C::QLANES + p * C::QROWS;
+            const bool there = row0 + local < rows;
+            const uint32_t flip = sbits ^ (shp.scale < 0.0f ? 0xffu : 0u);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t two = asked[p][0][e / 2], own = asked[p][e / 4][e % 4];
+                const uint32_t bits = shp.q_is_bf16 ? ((e & 1) ? two & 0xffff0000u : two << 16) : own;
+                x[e] = there ? __uint_as_float(bits ^ ((flip << (31 - e)) & 0x80000000u)) : 0.0f;
             }
-            float x[RPW][EPL];
 #pragma unroll
-            for (int r = 0; r < RPW; ++r) {
-                const int row = min(row0 + wave * RPW + r, rows - 1);
-                const int64_t sq = static_cast<int64_t>(seq) * shp.n_q + row / hpk;
-                const int64_t at = (sq * shp.n_q_heads + kvh * hpk + row % hpk) * D;
+            for (int m = 1; m < 8; m <<= 1)
 #pragma unroll
-                for (int j = 0; j < EPL; ++j) {
-                    const int64_t e = at + lane + 64 * j;
-                    x[r][j] = shp.q_is_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t *>(shp.q)[e]) << 16)
-                                            : static_cast<const float *>(shp.q)[e];
-                }
-            }
-            uint32_t neg[EPL];
-#pragma unroll
-            for (int j = 0; j < EPL; ++j) neg[j] = static_cast<uint32_t>(shp.signs[kvh * (D / 8) + (lane + 64 * j) / 8] >> (lane % 8)) << 31;
-#pragma unroll
-            for (int r = 0; r < RPW; ++r) {
-                const bool there = row0 + wave * RPW + r < rows;
-#pragma unroll
-                for (int j = 0; j < EPL; ++j) x[r][j] = there ? __uint_as_float(__float_as_uint(x[r][j]) ^ neg[j]) : 0.0f;
-            }
-            static_for<0, 6>([&](auto bb) {
+                for (int e = 0; e < 8; ++e)
+                    if ((e & m) == 0) {
+                        const float a = x[e], b = x[e | m];
+                        x[e] = a + b;
+                        x[e | m] = a - b;
+                    }
+            static_for<0, C::log2i(C::QLANES)>([&](auto bb) {
                 constexpr int m = 1 << decltype(bb)::value;
 #pragma unroll
-                for (int r = 0; r < RPW; ++r)
-#pragma unroll
-                    for (int j = 0; j < EPL; ++j) {
-                        const float other = lane_xor<m>(x[r][j], lane);
-                        x[r][j] = (lane & m) ? other - x[r][j] : x[r][j] + other;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const float other = lane_xor<m>(x[e], lane);
+                    x[e] = (lane & m) ? other - x[e] : x[e] + other;
+                }
             });
+            // a power of two brings the row's largest number into [1/2, 1): fp16 has no range to spare
+            float top = 0.0f;
 #pragma unroll
-            for (int m = 1; m < EPL; m <<= 1)
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+            static_for<0, C::log2i(C::QLANES)>([&](auto bb) { top = fmaxf(top, lane_xor<(1 << decltype(bb)::value)>(top, lane)); });
+            const int ex = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
+            if (C::ROWS % C::QROWS == 0 || local < C::ROWS) {
+                if (qc == 0) sm.factor[local] = ldexpf(norm, ex);
 #pragma unroll
-                for (int r = 0; r < RPW; ++r)
-#pragma unroll
-                    for (int j = 0; j < EPL; ++j)
-                        if ((j & m) == 0) {
-                            const float a = x[r][j], b = x[r][j | m];
-                            x[r][j] = a + b;
-                            x[r][j | m] = a - b;
-                        }
-#pragma unroll
-            for (int r = 0; r < RPW; ++r) {
-                // a power of two brings the row's largest number into [1/2, 1): fp16 has no range to spare
-                float top = 0.0f;
-#pragma unroll
-                for (int j = 0; j < EPL; ++j) top = fmaxf(top, fabsf(x[r][j]));
-                static_for<0, 6>([&](auto bb) { top = fmaxf(top, lane_xor<(1 << decltype(bb)::value)>(top, lane)); });
-                const int e = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
-                const int row = wave * RPW + r;
-                if (lane == 0) sm.factor[row] = ldexpf(norm, e);
-#pragma unroll
-                for (int j = 0; j < EPL; ++j) {
-                    const float y = ldexpf(x[r][j], -e);
-                    const _Float16 hi = static_cast<_Float16>(y);
-                    const _Float16 lo = static_cast<_Float16>(y - static_cast<float>(hi));
-                    unsigned char *to = qop + row * (4 * KS * 16) + slot[j];
+                for (int e = 0; e < 8; ++e) {
+                    const int c = 8 * qc + e, t = c / 3;
+                    const bool second = P::NCLASS == 2 && t >= P::NT0;
+                    const int of = second ? t - P::NT0 : t, each = second ? (C::T1 > 0 ? C::T1 : 1) : C::T0;
+                    const int at = of % each + (second ? C::T0 : 0);
+                    unsigned char *to = place + local * C::QST + ((of / each) * KS + at / 2) * 16 + ((at % 2) * 4 + c % 3) * 2;
+                    const float y = ldexpf(x[e], -ex);
+                    const _Float16 hi = static_cast<_Float16>(y), lo = static_cast<_Float16>(y - static_cast<float>(hi));
                     *reinterpret_cast<_Float16 *>(to) = hi;
-                    *reinterpret_cast<_Float16 *>(to + C::QOP) = lo;
+                    *reinterpret_cast<_Float16 *>(to + 4 * KS * 16) = lo;
                 }
             }
         }
         __syncthreads();
-        half8_t qh[2][KS], ql[2][KS];
-        float factor[2];
-        int limit[2];                    // tokens that the row sees
+        half8_t qh[RB][KS], ql[RB][KS];
+        float factor[RB];
+        int limit[RB];                   // tokens that the row sees
+        int all_see = len;               // tokens that every row sees
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-            const unsigned char *from = qop + ((rb * 16 + n) * 4 + g) * (KS * 16);
-#pragma unroll
-            for (int kk = 0; kk < KS; ++kk) {
-                qh[rb][kk] = *reinterpret_cast<const half8_t *>(from + kk * 16);
-                ql[rb][kk] = *reinterpret_cast<const half8_t *>(from + C::QOP + kk * 16);
-            }
+        for (int rb = 0; rb < RB; ++rb) {
+            // (places that no coordinate has: every fourth, those of triplets past a class's last and of coordinates past the last; what
+            // lies there is left over)
+            const unsigned char *from = place + (rb * 16 + n) * C::QST + g * (KS * 16);
+            static_for<0, KS>([&](auto kk_) {
+                constexpr int kk = decltype(kk_)::value;
+                uint4 h = *reinterpret_cast<const uint4 *>(from + kk * 16), l = *reinterpret_cast<const uint4 *>(from + 4 * KS * 16 + kk * 16);
+                auto keep = [&](auto at_, uint32_t &first, uint32_t &second) __attribute__((always_inline)) {
+                    constexpr int at = decltype(at_)::value;
+                    constexpr bool two = P::NCLASS == 2 && at >= C::T0;
+                    constexpr int each = two ? C::T1 : C::T0, count = two ? P::NT1 : P::NT0, within = two ? at - C::T0 : at;
+                    constexpr int base = two ? P::NT0 : 0;
+                    second &= 0xffffu;
+                    if constexpr (at >= C::TPL) {
+                        first = second = 0u;
+                    } else if constexpr (3 * each + within >= count - 1) {   // (some lane groups have none, or the last)
+                        const int t = g * each + within, left = t < count ? D - 3 * (base + t) : 0;   // coordinates of the triplet
+                        if (left < 3) second = 0u;
+                        if (left < 2) first &= 0xffffu;
+                        if (left < 1) first = 0u;
+                    }
+                };
+                keep(std::integral_constant<int, 2 * kk>{}, h.x, h.y);
+                keep(std::integral_constant<int, 2 * kk + 1>{}, h.z, h.w);
+                keep(std::integral_constant<int, 2 * kk>{}, l.x, l.y);
+                keep(std::integral_constant<int, 2 * kk + 1>{}, l.z, l.w);
+                qh[rb][kk] = __builtin_bit_cast(half8_t, h);
+                ql[rb][kk] = __builtin_bit_cast(half8_t, l);
+            });
             factor[rb] = sm.factor[rb * 16 + n];
             limit[rb] = len;
             const int row = row0 + rb * 16 + n;
             if (!shared && shp.causal && row < rows) {
                 const int nq = q_lens != nullptr ? min(max(q_lens[seq], 0), shp.n_q) : shp.n_q;
                 limit[rb] = min(max(len - nq + row / hpk + 1, 0), len);
+                all_see = min(max(len - nq + row0 / hpk + 1, 0), len);
             }
         }
-        __syncthreads();                 // the operands have been read: the staging areas are the wavefronts' own now
+        all_see = __builtin_amdgcn_readfirstlane(all_see);
+        __syncthreads();                 // the operands have been read: the values' places are the wavefronts' own now
+        if (work) load_values(begin + wave, page_of(begin + wave));
 
         // ---- the steps ----
-        float m_ref[2] = {-1e30f, -1e30f}, l_run[2] = {0.0f, 0.0f};   // (-1e30: no token seen yet)
-        f32x4_t oacc[2][CB];
+        float m_ref[RB], l_run[RB];
+        f32x4_t oacc[RB][CB];
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int rb = 0; rb < RB; ++rb) {
+            m_ref[rb] = -1e30f;          // (no token seen yet)
+            l_run[rb] = 0.0f;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
+        }
+        auto walk = [&](auto live_) __attribute__((always_inline)) {
+        constexpr int LIVE = decltype(live_)::value;   // blocks of 16 rows with rows
         for (int step = begin + wave; step < end; step += NW) {
             __builtin_amdgcn_wave_barrier();
-            store_step();
+            store_records();
             __builtin_amdgcn_wave_barrier();
-            if (step + NW < end) {
-                load_step(step + NW, next_page);
-                next_page = page_of(step + 2 * NW);
+            const bool more = step + NW < end;
+            if (more) {
+                if (step + NW - held_from >= 64 * NW) hold_pages(step + NW);
+                load_records(step + NW, page_of(step + NW));
             }
-            f32x4_t score[2][2];         // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
+            f32x4_t score[2][LIVE];      // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 uint32_t wd0[SD0::WORDS], wn0[SN0::WORDS];
@@ -369,7 +414,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     quarter(SD1{}, P::DIR1_BIT, DQ1, wd1, kb);
                     quarter(SN1{}, P::NRM1_BIT, NQ1, wn1, kb);
                 }
-                score[kb][0] = score[kb][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
                 static_for<0, KS>([&](auto kk_) {
                     constexpr int kk = decltype(kk_)::value;
                     auto entry = [&](auto at_) __attribute__((always_inline)) -> uint4 {
@@ -392,79 +438,116 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                             return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
                         }
                     };
-                    const uint4 a = entry(std::integral_constant<int, 2 * kk>{}), b = entry(std::integral_constant<int, 2 * kk + 1>{});
-                    const half8_t kh = __builtin_bit_cast(half8_t, make_uint4(a.x, a.y, b.x, b.y));
-                    const half8_t kl = __builtin_bit_cast(half8_t, make_uint4(a.z, a.w, b.z, b.w));
+                    // two entries (leading parts, remainders) to two operands: the halves in the middle change places
+                    uint4 a = entry(std::integral_constant<int, 2 * kk>{}), b = entry(std::integral_constant<int, 2 * kk + 1>{});
+                    asm("v_swap_b32 %0, %1" : "+v"(a.z), "+v"(b.x));
+                    asm("v_swap_b32 %0, %1" : "+v"(a.w), "+v"(b.y));
+                    const half8_t kh = __builtin_bit_cast(half8_t, a), kl = __builtin_bit_cast(half8_t, b);
 #pragma unroll
-                    for (int rb = 0; rb < 2; ++rb) {
-                        if (rb >= live) break;   // (uniform)
-                        score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[rb][kk], score[kb][rb], 0, 0, 0);
-                        score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[rb][kk], score[kb][rb], 0, 0, 0);
-                        score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[rb][kk], score[kb][rb], 0, 0, 0);
-                    }
+                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[rb][kk], score[kb][rb], 0, 0, 0);
+#pragma unroll
+                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[rb][kk], score[kb][rb], 0, 0, 0);
+#pragma unroll
+                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[rb][kk], score[kb][rb], 0, 0, 0);
                 });
+                float gamma[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) gamma[e] = *reinterpret_cast<const float *>(stage + (kb * 16 + 4 * g + e) * C::RST);
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) score[kb][rb][e] *= gamma[e];
             }
-            float gamma[2][4];
+            // tokens past the sequence's end, or that a row does not see for causality
+            if ((step + 1) * kPrefixKeys > all_see) {
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+                for (int rb = 0; rb < LIVE; ++rb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) gamma[kb][e] = *reinterpret_cast<const float *>(stage + (kb * 16 + 4 * g + e) * 16);
-
-            uint32_t ph[2][4], pl[2][4];
+                    for (int e = 0; e < 8; ++e)
+                        if (step * kPrefixKeys + (e / 4) * 16 + 4 * g + e % 4 >= limit[rb]) score[e / 4][rb][e % 4] = -INFINITY;
+            }
+            // probabilities are 2^(factor score - m_ref); a row's reference moves when a score exceeds it by more than 8
+            float top[LIVE];
+            bool higher = false;
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                if (rb >= live) break;
-                float t[8];
-                float top = -INFINITY;
+            for (int rb = 0; rb < LIVE; ++rb) {
+                top[rb] = score[0][rb][0];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    t[e] = score[e / 4][rb][e % 4] * gamma[e / 4][e % 4];
-                    const int tok = step * kPrefixKeys + (e / 4) * 16 + 4 * g + e % 4;
-                    t[e] = tok < limit[rb] ? t[e] * factor[rb] : -INFINITY;
-                    top = fmaxf(top, t[e]);
-                }
-                // probabilities are 2^(score - m_ref); the reference moves when a score exceeds it by more than 8
-                if (__ballot(top > m_ref[rb] + 8.0f) != 0) {
-                    top = fmaxf(top, lane_xor<16>(top, lane));
-                    top = fmaxf(top, lane_xor<32>(top, lane));
-                    const float m_new = fmaxf(m_ref[rb], top);
+                for (int e = 1; e < 8; ++e) top[rb] = fmaxf(top[rb], score[e / 4][rb][e % 4]);
+                top[rb] *= factor[rb];
+                higher = higher || top[rb] > m_ref[rb] + 8.0f;
+            }
+            if (__ballot(higher) != 0) {
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb) {
+                    top[rb] = fmaxf(top[rb], lane_xor<16>(top[rb], lane));
+                    top[rb] = fmaxf(top[rb], lane_xor<32>(top[rb], lane));
+                    const float m_new = fmaxf(m_ref[rb], top[rb]);
                     const float alpha = exp2_raw(m_ref[rb] - m_new);
                     m_ref[rb] = m_new;
                     l_run[rb] *= alpha;
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] *= alpha;
                 }
+            }
+            // the values have arrived (of what was asked for since, the next step's may be on their way); rows past the last token are
+            // made zeros: their probabilities are zero, but what lies there may be no number
+            if (more) wait_loads<C::NREC>(); else wait_loads<0>();
+            const int last = len - 1 - step * kPrefixKeys;
+            if (last < kPrefixKeys - 1) {
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float p0 = exp2_raw(t[e] - m_ref[rb]), p1 = exp2_raw(t[e + 1] - m_ref[rb]);
-                    l_run[rb] += p0 + p1;
-                    // two bf16 numbers whose sum is p to 2^-16: the values are bf16
-                    const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
-                    const float r0 = p0 - __uint_as_float(b0 & 0xffff0000u), r1 = p1 - __uint_as_float(b1 & 0xffff0000u);
-                    ph[rb][e / 2] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-                    pl[rb][e / 2] = bf16_rne(r0) | (bf16_rne(r1) << 16);
-                }
+                for (int e = 0; e < C::NVAL; ++e)
+                    if ((lane / LPR) * C::NVAL + e > last)
+                        *reinterpret_cast<uint4 *>(vals + e * C::VST + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
+                __builtin_amdgcn_wave_barrier();
             }
             // O^T += V^T P^T: k-slots 8 g .. + 3 are keys 4 g .. + 3 of the first block, the next four those of the second
             typedef __attribute__((address_space(3))) s16x4_t *tr_t;
+            const int row = 4 * g + n / 4;               // of the four that a lane group reads transposed, 16 channels of each
+            unsigned char *vat = vals + (row % C::NVAL) * C::VST + (row / C::NVAL) * (2 * D) + (n % 4) * 8;
+            constexpr int SECOND = (16 / C::NVAL) * (2 * D);   // 16 rows on
+            static_assert(16 % C::NVAL == 0, "16 rows on is a whole number of pieces on");
+            prefix_bf16x8_t p_hi[LIVE], p_lo[LIVE];
+#pragma unroll
+            for (int rb = 0; rb < LIVE; ++rb) {
+                uint32_t ph[4], pl[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = exp2_raw(fmaf(score[e / 4][rb][e % 4], factor[rb], -m_ref[rb]));
+                    const float p1 = exp2_raw(fmaf(score[e / 4][rb][e % 4 + 1], factor[rb], -m_ref[rb]));
+                    l_run[rb] += p0 + p1;
+                    // two bf16 numbers, each rounded to the nearest, whose sum is p to 2^-18: the values are bf16
+                    ph[e / 2] = bf16_pair(p0, p1);
+                    pl[e / 2] = bf16_pair(p0 - bf16_lo(ph[e / 2]), p1 - bf16_hi(ph[e / 2]));
+                }
+                p_hi[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[0], ph[1], ph[2], ph[3]));
+                p_lo[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+            }
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                unsigned char *at = stage + C::REC + (4 * g + n / 4) * C::VST + (16 * cb + 4 * (n % 4)) * 2;
                 union { s16x4_t h[2]; prefix_bf16x8_t b; } v;
-                v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)at);
-                v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(at + 16 * C::VST));
+                v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb));
+                v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb + SECOND));
 #pragma unroll
-                for (int rb = 0; rb < 2; ++rb) {
-                    if (rb >= live) break;
-                    oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[rb][0], ph[rb][1], ph[rb][2], ph[rb][3])), oacc[rb][cb], 0, 0, 0);
-                    oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[rb][0], pl[rb][1], pl[rb][2], pl[rb][3])), oacc[rb][cb], 0, 0, 0);
-                }
+                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, p_hi[rb], oacc[rb][cb], 0, 0, 0);
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, p_lo[rb], oacc[rb][cb], 0, 0, 0);
             }
+            wait_lds();                  // (the reads are done before anything new is asked for in their place)
+            if (more) load_values(step + NW, page_of(step + NW));
+        }
+        };
+        if (live > 2) {
+            if constexpr (RB > 2) walk(std::integral_constant<int, RB>{});
+        } else if (live == 2) {
+            walk(std::integral_constant<int, 2>{});
+        } else {
+            walk(std::integral_constant<int, 1>{});
         }
 
         // ---- the wavefronts' results join ----
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
+        for (int rb = 0; rb < RB; ++rb) {
             l_run[rb] += lane_xor<16>(l_run[rb], lane);
             l_run[rb] += lane_xor<32>(l_run[rb], lane);
             if (g == 0) {
@@ -473,11 +556,11 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
         }
         __syncthreads();                 // (the staging areas are free from here on, too)
-        float *out = reinterpret_cast<float *>(sm.stage[0]);   // [wavefront][16 rows][D]
+        float *out = reinterpret_cast<float *>(place);   // [wavefront][16 rows][OST]
         const int64_t prow0 = shared ? static_cast<int64_t>(kvh) * all_rows * splits
                                      : shp.own_partials + (static_cast<int64_t>(seq) * shp.n_kv_heads + kvh) * own_rows * splits;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
+        for (int rb = 0; rb < RB; ++rb) {
             if (rb >= live) break;
             float m_all = -1e30f;
 #pragma unroll
@@ -485,14 +568,14 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             const float weight = exp2_raw(m_ref[rb] - m_all);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
-                *reinterpret_cast<f32x4_t *>(out + (wave * 16 + n) * D + 16 * cb + 4 * g) = oacc[rb][cb] * weight;
+                *reinterpret_cast<f32x4_t *>(out + (wave * 16 + n) * C::OST + 16 * cb + 4 * g) = oacc[rb][cb] * weight;
             __syncthreads();
             for (int e = tid; e < 16 * D / 4; e += C::NT) {
                 const int r = e / (D / 4), row = row0 + rb * 16 + r;
                 if (row >= rows) continue;
                 f32x4_t sum = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int w = 0; w < NW; ++w) sum += *reinterpret_cast<const f32x4_t *>(out + (w * 16 + r) * D + (e % (D / 4)) * 4);
+                for (int w = 0; w < NW; ++w) sum += *reinterpret_cast<const f32x4_t *>(out + (w * 16 + r) * C::OST + (e % (D / 4)) * 4);
                 const int64_t prow = prow0 + static_cast<int64_t>(row) * splits + split;
                 *reinterpret_cast<f32x4_t *>(part_acc + prow * D + (e % (D / 4)) * 4) = sum;
                 if (e % (D / 4) == 0) {

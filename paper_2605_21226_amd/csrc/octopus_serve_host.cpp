@@ -42,8 +42,9 @@ PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t
     s.max_prefix = static_cast<int32_t>(max_prefix);
     s.max_len = static_cast<int32_t>(max_len);
     const int64_t hpk = n_q_heads / n_kv_heads, own_rows = n_q * hpk, all_rows = own_rows * n_seq;
-    s.prefix_groups = static_cast<int32_t>((all_rows + 31) / 32);
-    s.own_groups = static_cast<int32_t>((own_rows + 31) / 32);
+    const int64_t group = 32;                                         // query rows of a workgroup (PrefixCfg)
+    s.prefix_groups = static_cast<int32_t>((all_rows + group - 1) / group);
+    s.own_groups = static_cast<int32_t>((own_rows + group - 1) / group);
     const int64_t round_keys = 32 * (plan.head_dim <= 128 ? 8 : 4);
     const int64_t prefix_rounds = (max_prefix + round_keys - 1) / round_keys, own_rounds = (max_len + round_keys - 1) / round_keys;
     const int64_t prefix_units = static_cast<int64_t>(n_kv_heads) * s.prefix_groups, own_units = static_cast<int64_t>(n_seq) * n_kv_heads * s.own_groups;
@@ -52,8 +53,9 @@ PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t
     for (int64_t most = 1; most <= std::max<int64_t>(1, std::max(prefix_rounds, own_rounds)); most += std::max<int64_t>(1, most / 16)) {
         const int64_t a = ranges(prefix_rounds, most), b = ranges(own_rounds, most);
         const int64_t segments = prefix_units * a + own_units * b;
-        if (segments > INT32_MAX / 2 && most < std::max(prefix_rounds, own_rounds)) continue;
-        const double cost = static_cast<double>((segments + 255) / 256) * (2.5 + most) + static_cast<double>(all_rows) * n_kv_heads * (a + b) * 2e-5;
+        if (segments > INT32_MAX / 2) continue;
+        const int64_t longest = std::max(a > 0 ? (prefix_rounds + a - 1) / a : 0, b > 0 ? (own_rounds + b - 1) / b : 0);
+        const double cost = static_cast<double>((segments + 255) / 256) * (2.5 + longest) + static_cast<double>(all_rows) * n_kv_heads * (a + b) * 2e-5;
         if (cost < best) {
             best = cost;
             s.prefix_splits = static_cast<int32_t>(a);
@@ -102,7 +104,7 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb, const void *
         if (max_len > static_cast<int64_t>(max_pages_per_seq) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
     }
     if (q_dtype != OCTOPUS_DTYPE_F32 && q_dtype != OCTOPUS_DTYPE_BF16) return OCTOPUS_EUNSUPPORTED;
-    if (!aligned(q, q_dtype == OCTOPUS_DTYPE_F32 ? 4 : 2) || !aligned(out, 4) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
+    if (!aligned(q, 4) || !aligned(out, 4) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
         !aligned(q_lens, 4) || !std::isfinite(scale))
         return OCTOPUS_EINVAL;
     const size_t need = octopus_attn_prefix_workspace(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len);
