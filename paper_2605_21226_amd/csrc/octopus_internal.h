@@ -153,7 +153,9 @@ int launch_decode_vq(const octopus_codebooks_t &cb, const DecodeShape &s, const 
                      PageTable pt = PageTable{nullptr, 0, 0});   // pt: cache and vq are pools of pages
 
 // Attention of sequences that share a prefix (octopus_prefix.hpp).  A segment is one workgroup's share: a range of the prefix's or of a
-// sequence's tokens for 32 query rows of one KV head; the prefix's segments come first.
+// sequence's tokens for prefix_rows query rows of one KV head; the prefix's segments come first.
+constexpr int prefix_rows(int head_dim) { return head_dim <= 128 ? 32 : 16; }   // of a workgroup: what its registers hold
+constexpr int prefix_waves(int head_dim) { return head_dim <= 128 ? 8 : 4; }    // of a workgroup: what registers and LDS hold
 struct PrefixShape {
     int32_t n_seq, n_q_heads, n_kv_heads, n_q;
     int32_t max_prefix, max_len, max_pages, n_pages;
@@ -161,7 +163,7 @@ struct PrefixShape {
     const void *q;
     const uint8_t *signs;
     float scale;
-    int32_t prefix_groups, prefix_splits, own_groups, own_splits;   // groups of 32 rows, ranges of tokens
+    int32_t prefix_groups, prefix_splits, own_groups, own_splits;   // groups of query rows, ranges of tokens
     int32_t prefix_segments, n_segments;
     int64_t own_partials;   // partial results before the first of a sequence's own (one per query row and range)
 };

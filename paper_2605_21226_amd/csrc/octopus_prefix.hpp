@@ -32,8 +32,8 @@ struct PrefixCfg {
     static constexpr int D = P::D;
     // Wavefronts of a workgroup (two per SIMD, or one with all its registers) and blocks of 16 query rows of each: a key is decoded
     // once for a wavefront's rows.
-    static constexpr int NW = D <= 128 ? 8 : 4;
-    static constexpr int RB = 2;
+    static constexpr int NW = prefix_waves(D);
+    static constexpr int RB = prefix_rows(D) / 16;
     static constexpr int ROWS = 16 * RB;
     static constexpr int NT = kWave * NW;
     // triplets of each class that a lane group decodes; one class: padded to whole operands
@@ -46,8 +46,8 @@ struct PrefixCfg {
     static_assert(P::NCLASS == 1 || (J0 && J1), "two classes have joint tables");
     static constexpr int E0 = J0 ? 1 << (2 * P::BD0 + P::BN0) : 1 << (2 * P::BD0);
     static constexpr int E1 = P::NCLASS == 2 ? 1 << (2 * P::BD1 + P::BN1) : 0;
-    static constexpr int rep(int bytes, int budget) { return bytes * 8 <= budget ? 8 : (bytes * 4 <= budget ? 4 : (bytes * 2 <= budget ? 2 : 1)); }
-    static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : 65536);
+    static constexpr int rep(int bytes, int budget) { return bytes * 16 <= budget ? 16 : bytes * 8 <= budget ? 8 : (bytes * 4 <= budget ? 4 : (bytes * 2 <= budget ? 2 : 1)); }
+    static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : 65536);   // copies, 16 bytes apart
     static constexpr int R1 = P::NCLASS == 2 ? rep(E1 * 16, 16384) : 1;
     static constexpr int log2i(int x) { return x <= 1 ? 0 : 1 + log2i(x / 2); }
     static constexpr int RST = (P::GRANULES + 1) * 16;             // bytes of a staged record: keys that follow each other on other banks
@@ -416,30 +416,47 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 }
 #pragma unroll
                 for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                static_for<0, KS>([&](auto kk_) {
-                    constexpr int kk = decltype(kk_)::value;
-                    auto entry = [&](auto at_) __attribute__((always_inline)) -> uint4 {
-                        constexpr int at = decltype(at_)::value;
-                        if constexpr (at >= C::TPL) {
-                            return make_uint4(0u, 0u, 0u, 0u);
-                        } else if constexpr (at < C::T0) {
-                            const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0), nrm = field_clamped<at * P::BN0, P::BN0>(wn0);
-                            if constexpr (C::J0) {
-                                constexpr int NS = C::log2i(C::R0);
-                                return sm.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
-                            } else {
-                                const uint4 d4 = sm.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
-                                const float rho = sm.c_rho[0][nrm];
-                                return half_triplet(rho * __uint_as_float(d4.x), rho * __uint_as_float(d4.y), rho * __uint_as_float(d4.z));
-                            }
-                        } else if constexpr (P::NCLASS == 2) {
-                            constexpr int a1 = at - C::T0, NS = C::log2i(C::R1);
-                            const uint32_t dir = field_clamped<a1 * 2 * P::BD1, 2 * P::BD1>(wd1), nrm = field_clamped<a1 * P::BN1, P::BN1>(wn1);
-                            return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
+                auto entry = [&](auto at_) __attribute__((always_inline)) -> uint4 {
+                    constexpr int at = decltype(at_)::value;
+                    if constexpr (at >= C::TPL) {
+                        return make_uint4(0u, 0u, 0u, 0u);
+                    } else if constexpr (at < C::T0) {
+                        const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0), nrm = field_clamped<at * P::BN0, P::BN0>(wn0);
+                        if constexpr (C::J0 && 2 * P::BD0 == 8 && C::R0 * 16 << P::BN0 == 256) {
+                            // the code is a whole byte and the entry's offset has it as its second byte, above norm code and copy
+                            const uint32_t low = nrm << (4 + C::log2i(C::R0)) | static_cast<uint32_t>(lane & (C::R0 - 1)) << 4;
+                            const uint32_t at_byte = __builtin_amdgcn_perm(wd0[at / 4], low, 0x0c0c0400u + ((at % 4) << 8));
+                            return *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(sm.tab0) + at_byte);
+                        } else if constexpr (C::J0) {
+                            constexpr int NS = C::log2i(C::R0);
+                            return sm.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
+                        } else {
+                            const uint4 d4 = sm.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
+                            const float rho = sm.c_rho[0][nrm];
+                            return half_triplet(rho * __uint_as_float(d4.x), rho * __uint_as_float(d4.y), rho * __uint_as_float(d4.z));
                         }
-                    };
+                    } else if constexpr (P::NCLASS == 2) {
+                        constexpr int a1 = at - C::T0, NS = C::log2i(C::R1);
+                        const uint32_t dir = field_clamped<a1 * 2 * P::BD1, 2 * P::BD1>(wd1), nrm = field_clamped<a1 * P::BN1, P::BN1>(wn1);
+                        return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
+                    }
+                };
+                // (entries are asked for two operands ahead: LDS takes longer to answer than a product)
+                constexpr int AHEAD = 2;
+                uint4 ent[AHEAD + 1][2];
+                static_for<0, AHEAD>([&](auto kk_) {
+                    constexpr int kk = decltype(kk_)::value;
+                    ent[kk][0] = entry(std::integral_constant<int, 2 * kk>{});
+                    ent[kk][1] = entry(std::integral_constant<int, 2 * kk + 1>{});
+                });
+                static_for<0, KS>([&](auto kk_) {
+                    constexpr int kk = decltype(kk_)::value, next = kk + AHEAD;
+                    if constexpr (next < KS) {
+                        ent[next % (AHEAD + 1)][0] = entry(std::integral_constant<int, 2 * next>{});
+                        ent[next % (AHEAD + 1)][1] = entry(std::integral_constant<int, 2 * next + 1>{});
+                    }
+                    uint4 a = ent[kk % (AHEAD + 1)][0], b = ent[kk % (AHEAD + 1)][1];
                     // two entries (leading parts, remainders) to two operands: the halves in the middle change places
-                    uint4 a = entry(std::integral_constant<int, 2 * kk>{}), b = entry(std::integral_constant<int, 2 * kk + 1>{});
                     asm("v_swap_b32 %0, %1" : "+v"(a.z), "+v"(b.x));
                     asm("v_swap_b32 %0, %1" : "+v"(a.w), "+v"(b.y));
                     const half8_t kh = __builtin_bit_cast(half8_t, a), kl = __builtin_bit_cast(half8_t, b);
@@ -539,8 +556,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         };
         if (live > 2) {
             if constexpr (RB > 2) walk(std::integral_constant<int, RB>{});
-        } else if (live == 2) {
-            walk(std::integral_constant<int, 2>{});
+        } else if (RB > 1 && live == 2) {
+            if constexpr (RB > 1) walk(std::integral_constant<int, 2>{});
         } else {
             walk(std::integral_constant<int, 1>{});
         }

@@ -42,10 +42,10 @@ PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t
     s.max_prefix = static_cast<int32_t>(max_prefix);
     s.max_len = static_cast<int32_t>(max_len);
     const int64_t hpk = n_q_heads / n_kv_heads, own_rows = n_q * hpk, all_rows = own_rows * n_seq;
-    const int64_t group = 32;                                         // query rows of a workgroup (PrefixCfg)
+    const int64_t group = prefix_rows(plan.head_dim);
     s.prefix_groups = static_cast<int32_t>((all_rows + group - 1) / group);
     s.own_groups = static_cast<int32_t>((own_rows + group - 1) / group);
-    const int64_t round_keys = 32 * (plan.head_dim <= 128 ? 8 : 4);
+    const int64_t round_keys = 32 * prefix_waves(plan.head_dim);
     const int64_t prefix_rounds = (max_prefix + round_keys - 1) / round_keys, own_rounds = (max_len + round_keys - 1) / round_keys;
     const int64_t prefix_units = static_cast<int64_t>(n_kv_heads) * s.prefix_groups, own_units = static_cast<int64_t>(n_seq) * n_kv_heads * s.own_groups;
     auto ranges = [](int64_t rounds, int64_t most) { return rounds == 0 ? 0 : std::min<int64_t>((rounds + most - 1) / most, 128); };
@@ -54,8 +54,11 @@ PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t
         const int64_t a = ranges(prefix_rounds, most), b = ranges(own_rounds, most);
         const int64_t segments = prefix_units * a + own_units * b;
         if (segments > INT32_MAX / 2) continue;
-        const int64_t longest = std::max(a > 0 ? (prefix_rounds + a - 1) / a : 0, b > 0 ? (own_rounds + b - 1) / b : 0);
-        const double cost = static_cast<double>((segments + 255) / 256) * (2.5 + longest) + static_cast<double>(all_rows) * n_kv_heads * (a + b) * 2e-5;
+        // (a workgroup takes every 256th segment: the busiest has one of each kind too many, or none of the prefix's and one more own)
+        const double start = 2.5, shared = a > 0 ? start + (prefix_rounds + a - 1) / a : 0.0, mine = b > 0 ? start + (own_rounds + b - 1) / b : 0.0;
+        const int64_t n_shared = prefix_units * a, full = n_shared / 256, some = (n_shared + 255) / 256, all = (segments + 255) / 256;
+        const double cost = std::max(some * shared + std::max<int64_t>(all - some, 0) * mine, full * shared + (all - full) * mine) +
+                            static_cast<double>(all_rows) * n_kv_heads * (a + b) * 2e-5;
         if (cost < best) {
             best = cost;
             s.prefix_splits = static_cast<int32_t>(a);
