@@ -496,6 +496,65 @@ int octopus_attn_decode_paged_qjl(const octopus_codebooks_t *cb,
                                   void *workspace, size_t workspace_bytes,
                                   void *stream);
 
+/* ---- appending to pages, with the rotation by position (RoPE) ----
+ * A step's new keys, values and queries as the projection leaves them (views of one tensor, if need be), in one call:
+ * keys and queries are rotated by position, keys encoded into k_pool, values written into v_pool.
+ *   k, v         device, element (s, t, h, c) at s*stride_seq + t*stride_tok + h*stride_head + c; both kv_dtype F32/BF16; strides in
+ *                elements, multiples of 8, >= 0; bases 16-byte aligned.
+ *   new_lens     device int32 [n_seq] or NULL (all n_new): the tokens of each sequence that count (clamped to 0 .. n_new); a padded
+ *                batch's others are not looked at, their slots and their rows of q_out stay as they were.
+ *   rope         host, or NULL: no rotation.  At position p channels a, b of pair i < dim / 2 become a cos - b sin, a sin + b cos with
+ *                (cos, sin) = table[p][i]; pairs are channels i and i + dim / 2, or (interleaved) 2 i and 2 i + 1; channels from dim on
+ *                stay.  table: device fp32 [n_pos][dim / 2][2], 16-byte aligned; dim: a multiple of 16, <= head_dim; pos: device
+ *                int32 [n_seq], the position of each sequence's first new token, or NULL: its slot (start_pos), which is the
+ *                position where the cache holds the whole sequence; behind a shared prefix it is the slot plus the prefix's length.
+ *                A position outside [0, n_pos) is read as the nearest inside.  The rotation is computed in fp32 and the keys are
+ *                encoded as it leaves them (octopus_encode_paged of keys rotated in bf16 sees them rounded).
+ *   q            device, [n_seq][n_new][n_q_heads] rows like k (q_dtype, strides, alignment), or NULL: none.  q_out: device,
+ *                [n_seq][n_new][n_q_heads][d] contiguous, q_out_dtype F32/BF16, 16-byte aligned: the rotated queries (rope NULL: q
+ *                itself), as octopus_attn_decode_paged and octopus_attn_decode_paged_prefix take them.
+ *   signs, k_pool, n_pages, block_table, max_pages_per_seq, start_pos   as for octopus_encode_paged: token t of sequence s goes to slot
+ *                start_pos[s] + t; slots past max_pages_per_seq * 64 are not written.
+ *   v_pool       v_bits 0: bf16 pages [n_pages][n_kv_heads][64][d] (fp32 values are rounded to the nearest); v_bits 2..4: rows quantised
+ *                as by octopus_encode_values_paged(bits v_bits, group v_group), byte for byte.
+ * One launch; two with quantised values.  Codebooks: those octopus_build_codebooks returns (EUNSUPPORTED for edited ones).
+ * Errors: EINVAL (also n_seq or n_kv_heads above 65535, and more than 2^21 (tile, KV head, sequence) triples or runs of 16 tokens by
+ * eight rows), EUNSUPPORTED, EHIP. */
+typedef struct octopus_rope {
+    const float *table;
+    int64_t n_pos;
+    const int32_t *pos;
+    int32_t dim;
+    int32_t interleaved;
+} octopus_rope_t;
+
+int octopus_append_paged(const octopus_codebooks_t *cb,
+                         const void *k, int64_t k_stride_seq, int64_t k_stride_tok, int64_t k_stride_head,
+                         const void *v, int64_t v_stride_seq, int64_t v_stride_tok, int64_t v_stride_head, int32_t kv_dtype,
+                         int32_t n_seq, int32_t n_kv_heads, int32_t n_new, const int32_t *new_lens,
+                         const octopus_rope_t *rope,
+                         const void *q, int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head,
+                         int32_t n_q_heads, void *q_out, int32_t q_out_dtype,
+                         const uint8_t *signs,
+                         void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group, int32_t n_pages,
+                         const int32_t *block_table, int32_t max_pages_per_seq,
+                         const int32_t *start_pos,
+                         void *stream);
+
+/* ---- reading tokens of a paged cache back as values ----
+ * Rows t < lens[s] (clamped to 0 .. n_tok; NULL: all n_tok) of k_out and v_out, [n_seq][n_tok][n_kv_heads][d] contiguous, out_dtype
+ * F32/BF16, 16-byte aligned, become the keys k^ = gamma D_s H u^ that the records of slots start_pos[s] + t define (rotated by
+ * position if they were when they were encoded) and the value rows of those slots (dequantised where v_bits is 2..4); other rows,
+ * and slots past max_pages_per_seq * 64, are left as they were.  Either output may be NULL, and its pool then is not looked at (nor
+ * signs without keys).  Other arguments as for octopus_append_paged.
+ * Errors: EINVAL (also n_seq or n_kv_heads above 65535, and more than 2^23 (tile, KV head, sequence) triples), EUNSUPPORTED, EHIP. */
+int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
+                       const void *k_pool, const void *v_pool, int32_t v_bits, int32_t v_group, int32_t n_pages,
+                       const int32_t *block_table, int32_t max_pages_per_seq,
+                       int32_t n_seq, int32_t n_kv_heads, const int32_t *start_pos, int32_t n_tok, const int32_t *lens,
+                       void *k_out, void *v_out, int32_t out_dtype,
+                       void *stream);
+
 /* ---- sequences that share a prefix (the pages of octopus_encode_paged / octopus_attn_decode_paged) ----
  * A batch whose sequences all begin with the same tokens (a system prompt, the beams or samples of one prompt, drafts to be
  * verified) holds those tokens once, in pages of their own, and each sequence's other tokens in that sequence's pages:

@@ -27,7 +27,8 @@ EXPORTS = ("octopus_build_codebooks", "octopus_build_codebooks_pair", "octopus_c
            "octopus_attn_decode_paged_hybrid", "octopus_encode_values_paged", "octopus_attn_decode_paged_vq",
            "octopus_encode_qjl_paged", "octopus_attn_decode_paged_qjl",
            "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores",
-           "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix")
+           "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix",
+           "octopus_append_paged", "octopus_read_paged")
 
 
 class Plan(ctypes.Structure):
@@ -52,6 +53,16 @@ class Codebooks(ctypes.Structure):
         ("b_xi", (ctypes.c_float * MAX_LEVELS) * 2),
         ("c_rho", (ctypes.c_float * MAX_LEVELS) * 2),
         ("b_rho", (ctypes.c_float * MAX_LEVELS) * 2),
+    ]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("n_pos", ctypes.c_int64),
+        ("pos", ctypes.c_void_p),
+        ("dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
     ]
 
 
@@ -141,6 +152,11 @@ def load():
     lib.octopus_attn_decode_paged_prefix.argtypes = [CB, vp, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, i32, vp, i32, vp, i64, vp,
                                                      i32, vp, i64, f32, vp, vp, ctypes.c_size_t, vp]
     lib.octopus_attn_decode_paged_prefix.restype = ctypes.c_int
+    lib.octopus_append_paged.argtypes = [CB, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, i32, i32, vp, ctypes.POINTER(Rope), vp, i32,
+                                         i64, i64, i64, i32, vp, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp]
+    lib.octopus_append_paged.restype = ctypes.c_int
+    lib.octopus_read_paged.argtypes = [CB, vp, vp, vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, vp, vp, vp, i32, vp]
+    lib.octopus_read_paged.restype = ctypes.c_int
     lib.octopus_vq_on_matrix_cores.argtypes = [ctypes.POINTER(Codebooks), i32, i32, i32, i32, i32]
     lib.octopus_vq_on_matrix_cores.restype = ctypes.c_int
     lib.octopus_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
@@ -500,6 +516,46 @@ def octopus_attn_decode_paged_prefix(cb, q, signs, k_pool, v_pool, prefix_table,
         int(max_prefix), _ptr(block_table), 0 if block_table is None else block_table.shape[1], _ptr(seq_lens), int(max_len),
         float(scale), _ptr(out), _ptr(workspace), int(workspace.numel() * workspace.element_size()), _stream_ptr(stream))
     _check(code, "octopus_attn_decode_paged_prefix")
+
+
+def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos=None, new_lens=None, rope=None,
+                         rope_interleaved=False, rope_pos=None, q=None, q_out=None, v_bits=0, v_group=0, stream=None):
+    """A step's new tokens into pages: k and v device [n_seq, n_new, n_kv_heads, d] and q [n_seq, n_new, n_q_heads, d] (any strides with
+    contiguous channels; k and v of one type), rope device fp32 [n_pos, dim / 2, 2] contiguous (cos, sin) or None, rope_pos device
+    int32 [n_seq] or None (the slots), q_out device [n_seq, n_new, n_q_heads, d] contiguous, v_pool device bf16 pages or, with v_bits,
+    uint8 rows; start_pos and new_lens device int32 [n_seq] or None."""
+    assert k.dim() == 4 and k.stride(3) == 1 and v.stride(3) == 1 and v.shape == k.shape and v.dtype == k.dtype
+    n_seq, n_new, n_kv, d = k.shape
+    assert block_table.is_contiguous() and block_table.shape[0] == n_seq
+    turn = None
+    if rope is not None:
+        assert rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2 and _dtype_code(rope) == DTYPE_F32
+        turn = ctypes.byref(Rope(_ptr(rope), rope.shape[0], _ptr(rope_pos), 2 * rope.shape[1], int(bool(rope_interleaved))))
+    if q is not None:
+        assert q.stride(3) == 1 and q.shape[:2] == k.shape[:2] and q_out.is_contiguous() and q_out.shape == q.shape
+    code = load().octopus_append_paged(
+        ctypes.byref(cb), _ptr(k), k.stride(0), k.stride(1), k.stride(2), _ptr(v), v.stride(0), v.stride(1), v.stride(2), _dtype_code(k),
+        n_seq, n_kv, n_new, _ptr(new_lens), turn, _ptr(q), 0 if q is None else _dtype_code(q), 0 if q is None else q.stride(0),
+        0 if q is None else q.stride(1), 0 if q is None else q.stride(2), 0 if q is None else q.shape[2], _ptr(q_out),
+        0 if q_out is None else _dtype_code(q_out), _ptr(signs), _ptr(k_pool), _ptr(v_pool), int(v_bits), int(v_group), int(n_pages),
+        _ptr(block_table), int(block_table.shape[1]), _ptr(start_pos), _stream_ptr(stream))
+    _check(code, "octopus_append_paged")
+
+
+def octopus_read_paged(cb, signs, k_pool, v_pool, n_pages, block_table, k_out, v_out, start_pos=None, lens=None, v_bits=0, v_group=0,
+                       stream=None):
+    """Tokens start_pos[s] + t of a paged cache as values: k_out and v_out device [n_seq, n_tok, n_kv_heads, d] contiguous, of one
+    type (either may be None), lens device int32 [n_seq] or None."""
+    like = k_out if k_out is not None else v_out
+    n_seq, n_tok, n_kv, _ = like.shape
+    assert block_table.is_contiguous() and block_table.shape[0] == n_seq
+    for t in (k_out, v_out):
+        assert t is None or (t.is_contiguous() and t.shape == like.shape and t.dtype == like.dtype)
+    code = load().octopus_read_paged(
+        ctypes.byref(cb), _ptr(signs), _ptr(k_pool), _ptr(v_pool), int(v_bits), int(v_group), int(n_pages), _ptr(block_table),
+        int(block_table.shape[1]), n_seq, n_kv, _ptr(start_pos), n_tok, _ptr(lens), _ptr(k_out), _ptr(v_out), _dtype_code(like),
+        _stream_ptr(stream))
+    _check(code, "octopus_read_paged")
 
 
 def octopus_profile_events(before, after):

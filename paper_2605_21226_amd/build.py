@@ -20,7 +20,7 @@ for _d in ("256", "128", "64"):
                                                       "octopus_valu_d", "octopus_qjl_d", "octopus_enc_d", "octopus_round_d")]
     SOURCES += ["octopus_vqm_d" + _d + "_b" + _b + ".hip" for _b in ("4", "3", "2")]
 SOURCES += ["octopus_sweep_dec_d128.hip", "octopus_sweep_enc_d128.hip"]
-SOURCES += [_family + _d + ".hip" for _d in ("256", "128", "64") for _family in ("octopus_prefix_d",)]
+SOURCES += [_family + _d + ".hip" for _d in ("256", "128", "64") for _family in ("octopus_append_d", "octopus_prefix_d", "octopus_read_d")]
 SOURCES += ["octopus_common.hip", "octopus_values.hip", "octopus_serve.hip", "octopus_serve_host.cpp", "octopus_host.cpp"]
 # -packed-fp32-ops is switched off on purpose: hipcc must not form packed fp32 instructions here.
 FLAGS = (["-D" + d for d in os.environ.get("OCTOPUS_DEFS", "").split(",") if d]) + ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,

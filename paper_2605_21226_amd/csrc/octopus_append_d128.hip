@@ -1,0 +1,2 @@
+#define OCTOPUS_D 128
+#include "octopus_plans_append.inc"

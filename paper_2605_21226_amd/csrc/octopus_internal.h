@@ -176,6 +176,39 @@ int launch_prefix(const octopus_codebooks_t &cb, const PrefixShape &s, const voi
 int launch_prefix_merge(const octopus_plan_t &plan, const PrefixShape &s, const int32_t *prefix_len, const int32_t *seq_lens,
                         const int32_t *q_lens, const float *part_ml, const float *part_acc, float *out, void *stream);
 
+// Rotation by position: (cos, sin) pairs [n_pos][dim / 2]; table NULL: none.  pos (or NULL: the slot): position of a sequence's first
+// new token.
+struct RopeCall {
+    const float *table;
+    int64_t n_pos;
+    const int32_t *pos;
+    int32_t dim, interleaved;
+};
+// Appending to pages (octopus_append.hpp).  v_pool NULL: the values are quantised by a launch of their own; q NULL: no queries.
+struct AppendCall {
+    const void *k, *v, *q;
+    int64_t k_seq, k_tok, k_head, v_seq, v_tok, v_head, q_seq, q_tok, q_head;   // strides in elements
+    void *k_pool, *v_pool, *q_out;
+    const uint8_t *signs;
+    const int32_t *start_pos, *new_lens;
+    RopeCall rope;
+    PageTable pt;
+    int32_t n_seq, n_kv_heads, n_q_heads, n_new;
+    int32_t kv_is_bf16, q_is_bf16, q_out_is_bf16;
+};
+int launch_append(const octopus_codebooks_t &cb, const AppendCall &a, void *stream);
+int launch_append_values(const AppendCall &a, int32_t head_dim, int32_t bits, int32_t group, void *vq_pool, void *stream);
+// Reading back (octopus_read.hpp); k_out or v_out may be NULL.
+struct ReadCall {
+    const void *k_pool, *v_pool;
+    void *k_out, *v_out;
+    const uint8_t *signs;
+    const int32_t *start_pos, *lens;
+    PageTable pt;
+    int32_t n_seq, n_kv_heads, n_tok, v_bits, v_group, out_is_bf16;
+};
+int launch_read(const octopus_codebooks_t &cb, const ReadCall &a, void *stream);
+
 // What the entry points outside octopus_host.cpp ask of it: a plan whose parts fit together, codebooks the encoder takes, and the
 // measurement events armed for this thread's next decode-attention call (forgotten by the asking).
 bool plan_well_formed(const octopus_plan_t &plan);

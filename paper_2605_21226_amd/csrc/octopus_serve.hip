@@ -6,7 +6,9 @@ namespace octopus {
 
 #define OCTOPUS_DECL(D)                                                                                                   \
     int launch_prefix_d##D(const octopus_codebooks_t &, const PrefixShape &, const void *, const void *, const int32_t *, \
-                           const int32_t *, const int32_t *, const int32_t *, const int32_t *, float *, float *, void *);
+                           const int32_t *, const int32_t *, const int32_t *, const int32_t *, float *, float *, void *); \
+    int launch_append_d##D(const octopus_codebooks_t &, const AppendCall &, void *);                                      \
+    int launch_read_d##D(const octopus_codebooks_t &, const ReadCall &, void *);
 OCTOPUS_DECL(64)
 OCTOPUS_DECL(128)
 OCTOPUS_DECL(256)
@@ -25,6 +27,14 @@ int launch_prefix(const octopus_codebooks_t &cb, const PrefixShape &s, const voi
                   float *part_acc, void *stream) {
     OCTOPUS_BY_HEAD_DIM(cb.plan, launch_prefix, cb, s, k_pool, v_pool, prefix_table, prefix_len, block_table, seq_lens, q_lens, part_ml,
                         part_acc, stream)
+}
+
+int launch_append(const octopus_codebooks_t &cb, const AppendCall &a, void *stream) {
+    OCTOPUS_BY_HEAD_DIM(cb.plan, launch_append, cb, a, stream)
+}
+
+int launch_read(const octopus_codebooks_t &cb, const ReadCall &a, void *stream) {
+    OCTOPUS_BY_HEAD_DIM(cb.plan, launch_read, cb, a, stream)
 }
 
 // One wavefront per output row: out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over the row's partial results, the prefix's and

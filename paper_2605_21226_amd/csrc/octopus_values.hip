@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void encode_values_kernel(const void *__restri
                                                              int32_t n_kv_heads, int32_t n_new, int32_t d,
                                                              unsigned char *__restrict__ vq, int64_t t_capacity,
                                                              const int32_t *__restrict__ start_pos, int vec16,
-                                                             PageTable pt) {
+                                                             PageTable pt, const int32_t *__restrict__ new_lens) {
     constexpr int LEVELS = (1 << B) - 1;
     constexpr int CODE_WORDS = G * B / 32 + ((G * B) % 32 ? 1 : 0);   // 1, 2, 3 or 4
     constexpr int CODE_BYTES = G * B / 8;                             // the group's codes: 4 .. 16 bytes
@@ -46,6 +46,7 @@ __global__ __launch_bounds__(256) void encode_values_kernel(const void *__restri
     const int grp = static_cast<int>(r & static_cast<uint32_t>(n_groups - 1));
     const int kvh = static_cast<int>(r >> (31 - __builtin_clz(n_groups)));
     const int seq = blockIdx.z;
+    if (new_lens != nullptr && tok >= new_lens[seq]) return;   // (a padded batch: the sequence's rows end here)
     const int64_t pos = (start_pos ? max(start_pos[seq], 0) : 0) + tok;   // (a negative position would write before vq)
     if (pos >= t_capacity) return;
 
@@ -159,9 +160,9 @@ __global__ __launch_bounds__(256) void encode_values_kernel(const void *__restri
     *meta = make_float2(scale, lo);
 }
 
-int launch_encode_values(const void *v, int v_dtype, int64_t stride_seq, int64_t stride_tok, int64_t stride_head,
-                         int32_t n_seq, int32_t n_kv_heads, int32_t n_new, int32_t head_dim, int32_t bits,
-                         int32_t group, void *vq, int64_t t_capacity, const int32_t *start_pos, void *stream, PageTable pt) {
+static int encode_rows(const void *v, int v_dtype, int64_t stride_seq, int64_t stride_tok, int64_t stride_head,
+                       int32_t n_seq, int32_t n_kv_heads, int32_t n_new, int32_t head_dim, int32_t bits, int32_t group, void *vq,
+                       int64_t t_capacity, const int32_t *start_pos, void *stream, PageTable pt, const int32_t *new_lens) {
     const int64_t per_token = static_cast<int64_t>(n_kv_heads) * (head_dim / group);
     if (per_token > 4096 || n_seq > 65535) return static_cast<int>(hipErrorInvalidValue);
     if (n_seq == 0 || n_new == 0) return 0;
@@ -175,7 +176,7 @@ int launch_encode_values(const void *v, int v_dtype, int64_t stride_seq, int64_t
                        stride_head % per16 == 0) ? 1 : 0;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, v, stride_seq, stride_tok, stride_head, n_seq, n_kv_heads, n_new,
-                           head_dim, static_cast<unsigned char *>(vq), t_capacity, start_pos, vec16, pt);
+                           head_dim, static_cast<unsigned char *>(vq), t_capacity, start_pos, vec16, pt, new_lens);
     };
     const bool bf16 = v_dtype == OCTOPUS_DTYPE_BF16;
 #define OCTOPUS_CASE(B, G)                                                                                          \
@@ -186,6 +187,19 @@ int launch_encode_values(const void *v, int v_dtype, int64_t stride_seq, int64_t
     OCTOPUS_CASE(2, 16) OCTOPUS_CASE(3, 16) OCTOPUS_CASE(4, 16) OCTOPUS_CASE(2, 32) OCTOPUS_CASE(3, 32) OCTOPUS_CASE(4, 32)
 #undef OCTOPUS_CASE
     return static_cast<int>(hipErrorInvalidValue);
+}
+
+int launch_encode_values(const void *v, int v_dtype, int64_t stride_seq, int64_t stride_tok, int64_t stride_head,
+                         int32_t n_seq, int32_t n_kv_heads, int32_t n_new, int32_t head_dim, int32_t bits,
+                         int32_t group, void *vq, int64_t t_capacity, const int32_t *start_pos, void *stream, PageTable pt) {
+    return encode_rows(v, v_dtype, stride_seq, stride_tok, stride_head, n_seq, n_kv_heads, n_new, head_dim, bits, group, vq, t_capacity,
+                       start_pos, stream, pt, nullptr);
+}
+
+int launch_append_values(const AppendCall &a, int32_t head_dim, int32_t bits, int32_t group, void *vq_pool, void *stream) {
+    return encode_rows(a.v, a.kv_is_bf16 ? OCTOPUS_DTYPE_BF16 : OCTOPUS_DTYPE_F32, a.v_seq, a.v_tok, a.v_head, a.n_seq, a.n_kv_heads,
+                       a.n_new, head_dim, bits, group, vq_pool, static_cast<int64_t>(a.pt.stride) * OCTOPUS_TILE, a.start_pos, stream, a.pt,
+                       a.new_lens);
 }
 
 }  // namespace octopus
