@@ -518,27 +518,37 @@ def octopus_attn_decode_paged_prefix(cb, q, signs, k_pool, v_pool, prefix_table,
     _check(code, "octopus_attn_decode_paged_prefix")
 
 
+_NO_QUERIES = (None, 0, 0, 0, 0, 0, None, 0)
+
+
 def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos=None, new_lens=None, rope=None,
                          rope_interleaved=False, rope_pos=None, q=None, q_out=None, v_bits=0, v_group=0, stream=None):
     """A step's new tokens into pages: k and v device [n_seq, n_new, n_kv_heads, d] and q [n_seq, n_new, n_q_heads, d] (any strides with
     contiguous channels; k and v of one type), rope device fp32 [n_pos, dim / 2, 2] contiguous (cos, sin) or None, rope_pos device
     int32 [n_seq] or None (the slots), q_out device [n_seq, n_new, n_q_heads, d] contiguous, v_pool device bf16 pages or, with v_bits,
     uint8 rows; start_pos and new_lens device int32 [n_seq] or None."""
-    assert k.dim() == 4 and k.stride(3) == 1 and v.stride(3) == 1 and v.shape == k.shape and v.dtype == k.dtype
-    n_seq, n_new, n_kv, d = k.shape
+    n_seq, n_new, n_kv, _ = shape = k.shape
+    ks, kt, kh, kc = k.stride()
+    vs, vt, vh, vc = v.stride()
+    kind = _dtype_code(k)
+    assert kc == 1 and vc == 1 and v.shape == shape and _dtype_code(v) == kind
     assert block_table.is_contiguous() and block_table.shape[0] == n_seq
     turn = None
     if rope is not None:
-        assert rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2 and _dtype_code(rope) == DTYPE_F32
-        turn = ctypes.byref(Rope(_ptr(rope), rope.shape[0], _ptr(rope_pos), 2 * rope.shape[1], int(bool(rope_interleaved))))
+        n_pos, pairs, two = rope.shape
+        assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
+        turn = ctypes.byref(Rope(rope.data_ptr(), n_pos, _ptr(rope_pos), 2 * pairs, 1 if rope_interleaved else 0))
     if q is not None:
-        assert q.stride(3) == 1 and q.shape[:2] == k.shape[:2] and q_out.is_contiguous() and q_out.shape == q.shape
+        qs, qt, qh, qc = q.stride()
+        q_seq, q_new, n_qh, _ = q.shape
+        assert qc == 1 and q_seq == n_seq and q_new == n_new and q_out.is_contiguous() and q_out.shape == q.shape
+        q_args = (q.data_ptr(), _dtype_code(q), qs, qt, qh, n_qh, q_out.data_ptr(), _dtype_code(q_out))
+    else:
+        q_args = _NO_QUERIES
     code = load().octopus_append_paged(
-        ctypes.byref(cb), _ptr(k), k.stride(0), k.stride(1), k.stride(2), _ptr(v), v.stride(0), v.stride(1), v.stride(2), _dtype_code(k),
-        n_seq, n_kv, n_new, _ptr(new_lens), turn, _ptr(q), 0 if q is None else _dtype_code(q), 0 if q is None else q.stride(0),
-        0 if q is None else q.stride(1), 0 if q is None else q.stride(2), 0 if q is None else q.shape[2], _ptr(q_out),
-        0 if q_out is None else _dtype_code(q_out), _ptr(signs), _ptr(k_pool), _ptr(v_pool), int(v_bits), int(v_group), int(n_pages),
-        _ptr(block_table), int(block_table.shape[1]), _ptr(start_pos), _stream_ptr(stream))
+        ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, kind, n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
+        _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), block_table.shape[1], _ptr(start_pos),
+        _stream_ptr(stream))
     _check(code, "octopus_append_paged")
 
 

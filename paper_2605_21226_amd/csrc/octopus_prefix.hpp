@@ -163,15 +163,14 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     constexpr int64_t TILEB = P::GRANULES * kWave * 16, VTILEB = static_cast<int64_t>(kWave) * D * 2;
     __shared__ __attribute__((aligned(16))) PrefixSmem<P> sm;
     __shared__ __attribute__((aligned(16))) unsigned char place[C::PLACE];   // (an object of its own: reads of the tables need not wait for it)
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
 
     // levels, a lane each, then the tables
     {
         typedef const float __attribute__((address_space(4))) *arg_t;
         arg_t arg = (arg_t)__builtin_amdgcn_kernarg_segment_ptr();
         constexpr int NX = sizeof(sm.c_xi[0]) / 4, NR = sizeof(sm.c_rho[0]) / 4;
+        const int lane = threadIdx.x & 63;
         if (wave < P::NCLASS) {
             const float xi = arg[offsetof(DeviceBooks, c_xi) / 4 + wave * kMaxLevels + lane], rho = arg[offsetof(DeviceBooks, c_rho) / 4 + wave * kMaxLevels + lane];
             if (lane < NX) sm.c_xi[wave][lane] = xi;
@@ -179,7 +178,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         }
     }
     __syncthreads();
-    build_prefix_tables<P>(sm, tid);
+    build_prefix_tables<P>(sm, threadIdx.x);
 
     unsigned char *stage = sm.rec[wave], *vals = place + wave * C::VAL;
     constexpr int DQ0 = C::T0 * 2 * P::BD0, NQ0 = C::T0 * P::BN0, DQ1 = C::T1 * 2 * P::BD1, NQ1 = C::T1 * P::BN1;
@@ -187,23 +186,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     using SN0 = QuarterStream<P::NRM0_BIT, NQ0>;
     using SD1 = QuarterStream<P::DIR1_BIT, (DQ1 > 0 ? DQ1 : 32)>;
     using SN1 = QuarterStream<P::NRM1_BIT, (NQ1 > 0 ? NQ1 : 32)>;
-    // (the last quarter's padding may lie past the record, in the 16 bytes between two records or in the next: its terms meet zeros)
-    auto quarter = [&](auto stream_, int start, int quarter_bits, auto &words, int block) __attribute__((always_inline)) {
-        using S = decltype(stream_);
-        const int bit = start + g * quarter_bits;
-        const unsigned char *first = stage + n * C::RST + (bit >> 5) * 4 + block * (16 * C::RST);
-        uint32_t raw[S::READ];
-#pragma unroll
-        for (int j = 0; j < S::READ; ++j) raw[j] = *reinterpret_cast<const uint32_t *>(first + 4 * j);
-        if constexpr (S::ALIGNED) {
-#pragma unroll
-            for (int j = 0; j < S::WORDS; ++j) words[j] = raw[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < S::WORDS; ++j) words[j] = __builtin_amdgcn_alignbit(raw[j + 1], raw[j], bit & 31);
-        }
-    };
-
     const int hpk = shp.n_q_heads / shp.n_kv_heads;
     const int all_rows = shp.n_seq * shp.n_q * hpk, own_rows = shp.n_q * hpk;
     // what a factor of 256 in the keys and the units of log2 make of the caller's scale
@@ -211,6 +193,11 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     const float norm = fabsf(shp.scale) * kLog2e * (D == 64 ? 0.125f : (D == 128 ? 0.08838834764831845f : 0.0625f)) / kUnitScale;
 
     for (int seg = blockIdx.x; seg < shp.n_segments; seg += gridDim.x) {
+        // (opaque: what follows from a lane's number is computed for each segment, not kept -- in scratch memory, whose reads would
+        // wait for the values on their way -- from the kernel's start)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const int lane = tid & 63, n = lane & 15, g = lane >> 4;
         // ---- which (prefix or sequence, KV head, row group, split) this is ----
         const bool shared = seg < shp.prefix_segments;
         int i = shared ? seg : seg - shp.prefix_segments;
@@ -268,6 +255,23 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             hold_pages(begin + wave);
             load_records(begin + wave, page_of(begin + wave));
         }
+
+        // (the last quarter's padding may lie past the record, in the 16 bytes between two records or in the next: its terms meet zeros)
+        auto quarter = [&](auto stream_, int start, int quarter_bits, auto &words, int block) __attribute__((always_inline)) {
+            using S = decltype(stream_);
+            const int bit = start + g * quarter_bits;
+            const unsigned char *first = stage + n * C::RST + (bit >> 5) * 4 + block * (16 * C::RST);
+            uint32_t raw[S::READ];
+    #pragma unroll
+            for (int j = 0; j < S::READ; ++j) raw[j] = *reinterpret_cast<const uint32_t *>(first + 4 * j);
+            if constexpr (S::ALIGNED) {
+    #pragma unroll
+                for (int j = 0; j < S::WORDS; ++j) words[j] = raw[j];
+            } else {
+    #pragma unroll
+                for (int j = 0; j < S::WORDS; ++j) words[j] = __builtin_amdgcn_alignbit(raw[j + 1], raw[j], bit & 31);
+            }
+        };
 
         // ---- the segment's queries: asked for before the tables are complete, rotated, then as operands through LDS ----
         const int qc = tid % C::QLANES;                  // coordinates 8 qc .. + 7
@@ -335,12 +339,14 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
         }
         __syncthreads();
-        half8_t qh[RB][KS], ql[RB][KS];
-        float factor[RB];
-        int limit[RB];                   // tokens that the row sees
+        auto walk = [&](auto live_) __attribute__((always_inline)) {
+        constexpr int LIVE = decltype(live_)::value;   // blocks of 16 rows with rows
+        half8_t qh[LIVE][KS], ql[LIVE][KS];
+        float factor[LIVE];
+        int limit[LIVE];                   // tokens that the row sees
         int all_see = len;               // tokens that every row sees
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
+        for (int rb = 0; rb < LIVE; ++rb) {
             // (places that no coordinate has: every fourth, those of triplets past a class's last and of coordinates past the last; what
             // lies there is left over)
             const unsigned char *from = place + (rb * 16 + n) * C::QST + g * (KS * 16);
@@ -383,17 +389,15 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         if (work) load_values(begin + wave, page_of(begin + wave));
 
         // ---- the steps ----
-        float m_ref[RB], l_run[RB];
-        f32x4_t oacc[RB][CB];
+        float m_ref[LIVE], l_run[LIVE];
+        f32x4_t oacc[LIVE][CB];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
+        for (int rb = 0; rb < LIVE; ++rb) {
             m_ref[rb] = -1e30f;          // (no token seen yet)
             l_run[rb] = 0.0f;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        auto walk = [&](auto live_) __attribute__((always_inline)) {
-        constexpr int LIVE = decltype(live_)::value;   // blocks of 16 rows with rows
         for (int step = begin + wave; step < end; step += NW) {
             __builtin_amdgcn_wave_barrier();
             store_records();
@@ -553,18 +557,10 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             wait_lds();                  // (the reads are done before anything new is asked for in their place)
             if (more) load_values(step + NW, page_of(step + NW));
         }
-        };
-        if (live > 2) {
-            if constexpr (RB > 2) walk(std::integral_constant<int, RB>{});
-        } else if (RB > 1 && live == 2) {
-            if constexpr (RB > 1) walk(std::integral_constant<int, 2>{});
-        } else {
-            walk(std::integral_constant<int, 1>{});
-        }
 
         // ---- the wavefronts' results join ----
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
+        for (int rb = 0; rb < LIVE; ++rb) {
             l_run[rb] += lane_xor<16>(l_run[rb], lane);
             l_run[rb] += lane_xor<32>(l_run[rb], lane);
             if (g == 0) {
@@ -577,8 +573,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         const int64_t prow0 = shared ? static_cast<int64_t>(kvh) * all_rows * splits
                                      : shp.own_partials + (static_cast<int64_t>(seq) * shp.n_kv_heads + kvh) * own_rows * splits;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            if (rb >= live) break;
+        for (int rb = 0; rb < LIVE; ++rb) {
             float m_all = -1e30f;
 #pragma unroll
             for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, sm.ml[w][rb * 16 + n][0]);
@@ -607,6 +602,10 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
             __syncthreads();
         }
+        };
+        if (RB == 1 || live == 1) walk(std::integral_constant<int, 1>{});
+        else if (RB == 2 || live == 2) walk(std::integral_constant<int, (RB > 1 ? 2 : 1)>{});
+        else walk(std::integral_constant<int, RB>{});
     }
 }
 

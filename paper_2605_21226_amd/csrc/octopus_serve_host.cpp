@@ -137,7 +137,8 @@ int octopus_append_paged(const octopus_codebooks_t *cb, const void *k, int64_t k
                          int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head, int32_t n_q_heads, void *q_out,
                          int32_t q_out_dtype, const uint8_t *signs, void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group,
                          int32_t n_pages, const int32_t *block_table, int32_t max_pages_per_seq, const int32_t *start_pos, void *stream) {
-    if (cb == nullptr || k == nullptr || v == nullptr || signs == nullptr || k_pool == nullptr || v_pool == nullptr) return OCTOPUS_EINVAL;
+    if (cb == nullptr || signs == nullptr || k_pool == nullptr || v_pool == nullptr) return OCTOPUS_EINVAL;
+    if (n_new != 0 && (k == nullptr || v == nullptr)) return OCTOPUS_EINVAL;   // (an empty tensor may have no address)
     if (n_seq < 1 || n_kv_heads < 1 || n_new < 0 || n_seq > 65535 || n_kv_heads > 65535 || n_pages < 1) return OCTOPUS_EINVAL;
     if (!pages_ok(block_table, max_pages_per_seq) || !plan_well_formed(cb->plan)) return OCTOPUS_EINVAL;
     const int32_t d = cb->plan.head_dim;
@@ -201,7 +202,7 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs, cons
                        int32_t v_group, int32_t n_pages, const int32_t *block_table, int32_t max_pages_per_seq, int32_t n_seq,
                        int32_t n_kv_heads, const int32_t *start_pos, int32_t n_tok, const int32_t *lens, void *k_out, void *v_out,
                        int32_t out_dtype, void *stream) {
-    if (cb == nullptr || (k_out == nullptr && v_out == nullptr)) return OCTOPUS_EINVAL;
+    if (cb == nullptr || (n_tok != 0 && k_out == nullptr && v_out == nullptr)) return OCTOPUS_EINVAL;
     if ((k_out != nullptr && (k_pool == nullptr || signs == nullptr)) || (v_out != nullptr && v_pool == nullptr)) return OCTOPUS_EINVAL;
     if (n_seq < 1 || n_kv_heads < 1 || n_tok < 0 || n_seq > 65535 || n_kv_heads > 65535 || n_pages < 1) return OCTOPUS_EINVAL;
     if (!pages_ok(block_table, max_pages_per_seq) || !plan_well_formed(cb->plan)) return OCTOPUS_EINVAL;
