@@ -227,13 +227,13 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             return min(max(__builtin_amdgcn_readlane(held, (step - held_from) / NW), 0), shp.n_pages - 1);
         };
         constexpr bool HALF = P::GRANULES % 2 != 0;       // (an odd number of granules: the last piece is half the lanes')
-        const int rec_at = (lane / kPrefixKeys) * (kWave * 16) + (lane % kPrefixKeys) * 16;
+        const uint32_t rec_at = (lane / kPrefixKeys) * (kWave * 16) + (lane % kPrefixKeys) * 16;
         auto load_records = [&](int step, int page) __attribute__((always_inline)) {
             const unsigned char *src = k_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * TILEB + (step & 1) * (kPrefixKeys * 16);
 #pragma unroll
             for (int e = 0; e < C::NREC; ++e)
                 if (!HALF || e + 1 < C::NREC || lane < 32)
-                    rec[e] = *reinterpret_cast<const prefix_u32x4_t *>(src + e * (2 * kWave * 16) + rec_at);
+                    rec[e] = *reinterpret_cast<const prefix_u32x4_t *>(src + (rec_at + e * (2 * kWave * 16)));
         };
         auto store_records = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -242,12 +242,12 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     *reinterpret_cast<prefix_u32x4_t *>(stage + (lane % kPrefixKeys) * C::RST + (lane / kPrefixKeys + 2 * e) * 16) = rec[e];
         };
         constexpr int LPR = D / 8;                       // lanes per value row
-        const int val_at = (lane / LPR) * (C::NVAL * 2 * D) + (lane % LPR) * 16;
+        const uint32_t val_at = (lane / LPR) * (C::NVAL * 2 * D) + (lane % LPR) * 16;
         auto load_values = [&](int step, int page) __attribute__((always_inline)) {
-            const unsigned char *src = v_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * VTILEB + (step & 1) * (kPrefixKeys * 2 * D) + val_at;
+            const unsigned char *src = v_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * VTILEB + (step & 1) * (kPrefixKeys * 2 * D);
 #pragma unroll
             for (int e = 0; e < C::NVAL; ++e)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + e * (2 * D)),
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (val_at + e * (2 * D))),
                                                  (__attribute__((address_space(3))) void *)(vals + e * C::VST), 16, 0, 0);
         };
         const bool work = begin + wave < end;
@@ -398,86 +398,108 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        for (int step = begin + wave; step < end; step += NW) {
-            __builtin_amdgcn_wave_barrier();
-            store_records();
-            __builtin_amdgcn_wave_barrier();
-            const bool more = step + NW < end;
-            if (more) {
-                if (step + NW - held_from >= 64 * NW) hold_pages(step + NW);
-                load_records(step + NW, page_of(step + NW));
-            }
-            f32x4_t score[2][LIVE];      // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
+        // the code words of a step's keys n and 16 + n
+        uint32_t wd0[2][SD0::WORDS], wn0[2][SN0::WORDS];
+        [[maybe_unused]] uint32_t wd1[2][SD1::WORDS], wn1[2][SN1::WORDS];
+        auto read_words = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                uint32_t wd0[SD0::WORDS], wn0[SN0::WORDS];
-                quarter(SD0{}, P::DIR0_BIT, DQ0, wd0, kb);
-                quarter(SN0{}, P::NRM0_BIT, NQ0, wn0, kb);
-                [[maybe_unused]] uint32_t wd1[SD1::WORDS], wn1[SN1::WORDS];
+                quarter(SD0{}, P::DIR0_BIT, DQ0, wd0[kb], kb);
+                quarter(SN0{}, P::NRM0_BIT, NQ0, wn0[kb], kb);
                 if constexpr (P::NCLASS == 2) {
-                    quarter(SD1{}, P::DIR1_BIT, DQ1, wd1, kb);
-                    quarter(SN1{}, P::NRM1_BIT, NQ1, wn1, kb);
+                    quarter(SD1{}, P::DIR1_BIT, DQ1, wd1[kb], kb);
+                    quarter(SN1{}, P::NRM1_BIT, NQ1, wn1[kb], kb);
                 }
-#pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                auto entry = [&](auto at_) __attribute__((always_inline)) -> uint4 {
-                    constexpr int at = decltype(at_)::value;
-                    if constexpr (at >= C::TPL) {
-                        return make_uint4(0u, 0u, 0u, 0u);
-                    } else if constexpr (at < C::T0) {
-                        const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0), nrm = field_clamped<at * P::BN0, P::BN0>(wn0);
-                        if constexpr (C::J0 && 2 * P::BD0 == 8 && C::R0 * 16 << P::BN0 == 256) {
-                            // the code is a whole byte and the entry's offset has it as its second byte, above norm code and copy
-                            const uint32_t low = nrm << (4 + C::log2i(C::R0)) | static_cast<uint32_t>(lane & (C::R0 - 1)) << 4;
-                            const uint32_t at_byte = __builtin_amdgcn_perm(wd0[at / 4], low, 0x0c0c0400u + ((at % 4) << 8));
-                            return *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(sm.tab0) + at_byte);
-                        } else if constexpr (C::J0) {
-                            constexpr int NS = C::log2i(C::R0);
-                            return sm.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
-                        } else {
-                            const uint4 d4 = sm.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
-                            const float rho = sm.c_rho[0][nrm];
-                            return half_triplet(rho * __uint_as_float(d4.x), rho * __uint_as_float(d4.y), rho * __uint_as_float(d4.z));
-                        }
-                    } else if constexpr (P::NCLASS == 2) {
-                        constexpr int a1 = at - C::T0, NS = C::log2i(C::R1);
-                        const uint32_t dir = field_clamped<a1 * 2 * P::BD1, 2 * P::BD1>(wd1), nrm = field_clamped<a1 * P::BN1, P::BN1>(wn1);
-                        return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
+            }
+        };
+        if (work) {
+            store_records();
+            __builtin_amdgcn_wave_barrier();
+            if (begin + wave + NW < end) load_records(begin + wave + NW, page_of(begin + wave + NW));
+            read_words();
+        }
+        for (int step = begin + wave; step < end; step += NW) {
+            const bool more = step + NW < end, two_more = step + 2 * NW < end;
+            f32x4_t score[2][LIVE];      // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
+            float gamma[2][4];
+            // An operand (two triplets) of a key block at a time; the entries of the next one are asked for before the products of this
+            // one, as LDS takes longer to answer than a product.
+            auto entry = [&](auto kb_, auto at_) __attribute__((always_inline)) -> uint4 {
+                constexpr int kb = decltype(kb_)::value, at = decltype(at_)::value;
+                if constexpr (at >= C::TPL) {
+                    return make_uint4(0u, 0u, 0u, 0u);
+                } else if constexpr (at < C::T0) {
+                    const uint32_t nrm = field_clamped<at * P::BN0, P::BN0>(wn0[kb]);
+                    if constexpr (C::J0 && 2 * P::BD0 == 8 && C::R0 * 16 << P::BN0 == 256) {
+                        // the code is a whole byte and the entry's offset has it as its second byte, above norm code and copy
+                        const uint32_t low = nrm << (4 + C::log2i(C::R0)) | static_cast<uint32_t>(lane & (C::R0 - 1)) << 4;
+                        const uint32_t at_byte = __builtin_amdgcn_perm(wd0[kb][at / 4], low, 0x0c0c0400u + ((at % 4) << 8));
+                        return *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(sm.tab0) + at_byte);
+                    } else if constexpr (C::J0) {
+                        constexpr int NS = C::log2i(C::R0);
+                        const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0[kb]);
+                        return sm.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
+                    } else {
+                        const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0[kb]);
+                        uint4 d4 = sm.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
+                        d4.w = __float_as_uint(sm.c_rho[0][nrm]);
+                        return d4;
                     }
-                };
-                // (entries are asked for two operands ahead: LDS takes longer to answer than a product)
-                constexpr int AHEAD = 2;
-                uint4 ent[AHEAD + 1][2];
-                static_for<0, AHEAD>([&](auto kk_) {
-                    constexpr int kk = decltype(kk_)::value;
-                    ent[kk][0] = entry(std::integral_constant<int, 2 * kk>{});
-                    ent[kk][1] = entry(std::integral_constant<int, 2 * kk + 1>{});
-                });
-                static_for<0, KS>([&](auto kk_) {
-                    constexpr int kk = decltype(kk_)::value, next = kk + AHEAD;
-                    if constexpr (next < KS) {
-                        ent[next % (AHEAD + 1)][0] = entry(std::integral_constant<int, 2 * next>{});
-                        ent[next % (AHEAD + 1)][1] = entry(std::integral_constant<int, 2 * next + 1>{});
-                    }
-                    uint4 a = ent[kk % (AHEAD + 1)][0], b = ent[kk % (AHEAD + 1)][1];
-                    // two entries (leading parts, remainders) to two operands: the halves in the middle change places
-                    asm("v_swap_b32 %0, %1" : "+v"(a.z), "+v"(b.x));
-                    asm("v_swap_b32 %0, %1" : "+v"(a.w), "+v"(b.y));
-                    const half8_t kh = __builtin_bit_cast(half8_t, a), kl = __builtin_bit_cast(half8_t, b);
+                } else if constexpr (P::NCLASS == 2) {
+                    constexpr int a1 = at - C::T0, NS = C::log2i(C::R1);
+                    const uint32_t dir = field_clamped<a1 * 2 * P::BD1, 2 * P::BD1>(wd1[kb]), nrm = field_clamped<a1 * P::BN1, P::BN1>(wn1[kb]);
+                    return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
+                }
+            };
+            // (tables without norms: the triplet is put together here)
+            auto triplet = [&](uint4 e) __attribute__((always_inline)) -> uint4 {
+                if constexpr (C::J0) return e;
+                const float rho = __uint_as_float(e.w);
+                return half_triplet(rho * __uint_as_float(e.x), rho * __uint_as_float(e.y), rho * __uint_as_float(e.z));
+            };
+            uint4 ent[2][2];
+            auto ask = [&](auto s_) __attribute__((always_inline)) {
+                constexpr int s = decltype(s_)::value, kb = s / KS, kk = s % KS;
+                ent[s % 2][0] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk>{});
+                ent[s % 2][1] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk + 1>{});
+            };
+            ask(std::integral_constant<int, 0>{});
+            static_for<0, 2 * KS>([&](auto s_) {
+                constexpr int s = decltype(s_)::value, kb = s / KS, kk = s % KS;
+                if constexpr (s + 1 < 2 * KS) {
+                    ask(std::integral_constant<int, s + 1>{});
+                } else {
 #pragma unroll
-                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[rb][kk], score[kb][rb], 0, 0, 0);
-#pragma unroll
-                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[rb][kk], score[kb][rb], 0, 0, 0);
-#pragma unroll
-                    for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[rb][kk], score[kb][rb], 0, 0, 0);
-                });
-                float gamma[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) gamma[e] = *reinterpret_cast<const float *>(stage + (kb * 16 + 4 * g + e) * C::RST);
+                    for (int e = 0; e < 8; ++e) gamma[e / 4][e % 4] = *reinterpret_cast<const float *>(stage + ((e / 4) * 16 + 4 * g + e % 4) * C::RST);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // two entries (leading parts, remainders) to two operands: the halves in the middle change places
+                uint4 a = triplet(ent[s % 2][0]), b = triplet(ent[s % 2][1]);
+                asm("v_swap_b32 %0, %1" : "+v"(a.z), "+v"(b.x));
+                asm("v_swap_b32 %0, %1" : "+v"(a.w), "+v"(b.y));
+                const half8_t kh = __builtin_bit_cast(half8_t, a), kl = __builtin_bit_cast(half8_t, b);
 #pragma unroll
                 for (int rb = 0; rb < LIVE; ++rb)
+                    score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[rb][kk], kk == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : score[kb][rb], 0, 0, 0);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) score[kb][rb][e] *= gamma[e];
+                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[rb][kk], score[kb][rb], 0, 0, 0);
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[rb][kk], score[kb][rb], 0, 0, 0);
+            });
+#pragma unroll
+            for (int rb = 0; rb < LIVE; ++rb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) score[e / 4][rb][e % 4] *= gamma[e / 4][e % 4];
+            // nothing reads this step's records any more: the next step's take their place, the ones after that are asked for
+            if (more) {
+                __builtin_amdgcn_wave_barrier();
+                store_records();
+                __builtin_amdgcn_wave_barrier();
+                if (two_more) {
+                    if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
+                    load_records(step + 2 * NW, page_of(step + 2 * NW));
+                }
+                read_words();
             }
             // tokens past the sequence's end, or that a row does not see for causality
             if ((step + 1) * kPrefixKeys > all_see) {
@@ -513,7 +535,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
             // the values have arrived (of what was asked for since, the next step's may be on their way); rows past the last token are
             // made zeros: their probabilities are zero, but what lies there may be no number
-            if (more) wait_loads<C::NREC>(); else wait_loads<0>();
+            if (two_more) wait_loads<C::NREC>(); else wait_loads<0>();
             const int last = len - 1 - step * kPrefixKeys;
             if (last < kPrefixKeys - 1) {
 #pragma unroll
