@@ -200,7 +200,13 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         const int lane = tid & 63, n = lane & 15, g = lane >> 4;
         // ---- which (prefix or sequence, KV head, row group, split) this is ----
         const bool shared = seg < shp.prefix_segments;
-        int i = shared ? seg : seg - shp.prefix_segments;
+        // (neighbours in the grid lie on different dies: each die takes a run of the prefix's segments, so that the row groups that read
+        // the same tokens find them in its L2 cache)
+        int i = seg - shp.prefix_segments;
+        if (shared) {
+            const int die = seg % 8, each = shp.prefix_segments / 8, more = shp.prefix_segments % 8;
+            i = die * each + min(die, more) + seg / 8;
+        }
         const int groups = shared ? shp.prefix_groups : shp.own_groups, splits = shared ? shp.prefix_splits : shp.own_splits;
         const int grp = i % groups;
         i /= groups;
@@ -386,7 +392,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         }
         all_see = __builtin_amdgcn_readfirstlane(all_see);
         __syncthreads();                 // the operands have been read: the values' places are the wavefronts' own now
-        if (work) load_values(begin + wave, page_of(begin + wave));
 
         // ---- the steps ----
         float m_ref[LIVE], l_run[LIVE];
@@ -416,6 +421,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             store_records();
             __builtin_amdgcn_wave_barrier();
             if (begin + wave + NW < end) load_records(begin + wave + NW, page_of(begin + wave + NW));
+            load_values(begin + wave, page_of(begin + wave));    // (after the records, which are waited for first)
             read_words();
         }
         for (int step = begin + wave; step < end; step += NW) {
@@ -490,15 +496,11 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             for (int rb = 0; rb < LIVE; ++rb)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) score[e / 4][rb][e % 4] *= gamma[e / 4][e % 4];
-            // nothing reads this step's records any more: the next step's take their place, the ones after that are asked for
+            // nothing reads this step's records any more: the next step's take their place
             if (more) {
                 __builtin_amdgcn_wave_barrier();
                 store_records();
                 __builtin_amdgcn_wave_barrier();
-                if (two_more) {
-                    if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
-                    load_records(step + 2 * NW, page_of(step + 2 * NW));
-                }
                 read_words();
             }
             // tokens past the sequence's end, or that a row does not see for causality
@@ -533,9 +535,14 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] *= alpha;
                 }
             }
-            // the values have arrived (of what was asked for since, the next step's may be on their way); rows past the last token are
-            // made zeros: their probabilities are zero, but what lies there may be no number
-            if (two_more) wait_loads<C::NREC>(); else wait_loads<0>();
+            // The values have arrived; the records of the step after the next are asked for only now, as waiting for what a load
+            // wrote to LDS waits for every load. Rows past the last token are made zeros: their probabilities are zero, but what
+            // lies there may be no number.
+            wait_loads<0>();
+            if (two_more) {
+                if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
+                load_records(step + 2 * NW, page_of(step + 2 * NW));
+            }
             const int last = len - 1 - step * kPrefixKeys;
             if (last < kPrefixKeys - 1) {
 #pragma unroll
@@ -545,6 +552,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 __builtin_amdgcn_wave_barrier();
             }
             // O^T += V^T P^T: k-slots 8 g .. + 3 are keys 4 g .. + 3 of the first block, the next four those of the second
+            constexpr int AHEAD_V = 3;                   // (channels of this and the next two products are held)
             typedef __attribute__((address_space(3))) s16x4_t *tr_t;
             const int row = 4 * g + n / 4;               // of the four that a lane group reads transposed, 16 channels of each
             unsigned char *vat = vals + (row % C::NVAL) * C::VST + (row / C::NVAL) * (2 * D) + (n % 4) * 8;
@@ -566,15 +574,21 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 p_hi[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[0], ph[1], ph[2], ph[3]));
                 p_lo[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
             }
+            union channels_t { s16x4_t h[2]; prefix_bf16x8_t b; } v[AHEAD_V];
+            auto ask_values = [&](int cb) __attribute__((always_inline)) {
+                v[cb % AHEAD_V].h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb));
+                v[cb % AHEAD_V].h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb + SECOND));
+            };
+#pragma unroll
+            for (int cb = 0; cb < AHEAD_V - 1; ++cb) ask_values(cb);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                union { s16x4_t h[2]; prefix_bf16x8_t b; } v;
-                v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb));
-                v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb + SECOND));
+                if (cb + AHEAD_V - 1 < CB) ask_values(cb + AHEAD_V - 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, p_hi[rb], oacc[rb][cb], 0, 0, 0);
+                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_hi[rb], oacc[rb][cb], 0, 0, 0);
 #pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.b, p_lo[rb], oacc[rb][cb], 0, 0, 0);
+                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_lo[rb], oacc[rb][cb], 0, 0, 0);
             }
             wait_lds();                  // (the reads are done before anything new is asked for in their place)
             if (more) load_values(step + NW, page_of(step + NW));
