@@ -47,16 +47,17 @@ struct PrefixCfg {
     static constexpr int E0 = J0 ? 1 << (2 * P::BD0 + P::BN0) : 1 << (2 * P::BD0);
     static constexpr int E1 = P::NCLASS == 2 ? 1 << (2 * P::BD1 + P::BN1) : 0;
     static constexpr int rep(int bytes, int budget) { return bytes * 16 <= budget ? 16 : bytes * 8 <= budget ? 8 : (bytes * 4 <= budget ? 4 : (bytes * 2 <= budget ? 2 : 1)); }
-    static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : 65536);   // copies, 16 bytes apart
-    static constexpr int R1 = P::NCLASS == 2 ? rep(E1 * 16, 16384) : 1;
     static constexpr int log2i(int x) { return x <= 1 ? 0 : 1 + log2i(x / 2); }
-    static constexpr int RST = (P::GRANULES + 1) * 16;             // bytes of a staged record: keys that follow each other on other banks
+    // bytes of a staged record, an odd number of sixteens: 16 keys' words at one place of the record lie on 16 different sets of banks
+    // (at head dimension 256 eight sixteens cost 2000 clocks a step, a quarter of it)
+    static constexpr int RST = ((P::GRANULES + 1) | 1) * 16;
     static constexpr int REC = RST * kPrefixKeys;                  // bytes of a step's records
     static constexpr int NREC = (P::GRANULES + 1) / 2;              // 16-byte pieces per lane
     // A step's value rows go from memory to LDS directly, 1 KB per instruction: instruction i takes rows i, i + NVAL, ..; 32 bytes
     // between the instructions' pieces put four rows that follow each other on 32 different banks (the transposed reads take four).
     static constexpr int NVAL = D / 16;
     static constexpr int VST = 1024 + 32;
+    static constexpr bool VREG = D != 128;
     static constexpr int VAL = NVAL * VST;                         // bytes of a step's values
     // Query operands in LDS: a row's leading parts and its remainders; rows 16 bytes apart beyond their size, so that the 16 rows read
     // at once lie on all banks.  The wavefronts' results: rows 16 bytes apart for the same reason.  Both take the values' place.
@@ -64,6 +65,10 @@ struct PrefixCfg {
     static constexpr int OST = D + 4;                              // floats
     static constexpr int PLACE = (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL) > NW * 16 * OST * 4 ? (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL)
                                                                                                : NW * 16 * OST * 4;
+    // Copies of the tables' entries, 16 bytes apart, in what is left of LDS (4 KB of it for what is small).
+    static constexpr int LEFT = 160 * 1024 - PLACE - NW * REC - 4096;
+    static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : (LEFT < 65536 ? LEFT : 65536));
+    static constexpr int R1 = P::NCLASS == 2 ? rep(E1 * 16, 16384) : 1;
     // The transform of the queries: eight coordinates a thread.
     static constexpr int QLANES = D / 8, QROWS = NT / QLANES, QPASS = (ROWS + QROWS - 1) / QROWS;
 };
@@ -249,17 +254,26 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         };
         constexpr int LPR = D / 8;                       // lanes per value row
         const uint32_t val_at = (lane / LPR) * (C::NVAL * 2 * D) + (lane % LPR) * 16;
+        [[maybe_unused]] prefix_u32x4_t val[C::VREG ? C::NVAL : 1];
         auto load_values = [&](int step, int page) __attribute__((always_inline)) {
             const unsigned char *src = v_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * VTILEB + (step & 1) * (kPrefixKeys * 2 * D);
 #pragma unroll
             for (int e = 0; e < C::NVAL; ++e)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (val_at + e * (2 * D))),
-                                                 (__attribute__((address_space(3))) void *)(vals + e * C::VST), 16, 0, 0);
+                if constexpr (C::VREG)
+                    val[e] = *reinterpret_cast<const prefix_u32x4_t *>(src + (val_at + e * (2 * D)));
+                else
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (val_at + e * (2 * D))),
+                                                     (__attribute__((address_space(3))) void *)(vals + e * C::VST), 16, 0, 0);
+        };
+        [[maybe_unused]] auto store_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < C::NVAL; ++e) *reinterpret_cast<prefix_u32x4_t *>(vals + e * C::VST + lane * 16) = val[e];
         };
         const bool work = begin + wave < end;
         if (work) {
             hold_pages(begin + wave);
             load_records(begin + wave, page_of(begin + wave));
+            if constexpr (C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
 
         // (the last quarter's padding may lie past the record, in the 16 bytes between two records or in the next: its terms meet zeros)
@@ -420,9 +434,13 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         if (work) {
             store_records();
             __builtin_amdgcn_wave_barrier();
-            if (begin + wave + NW < end) load_records(begin + wave + NW, page_of(begin + wave + NW));
-            load_values(begin + wave, page_of(begin + wave));    // (after the records, which are waited for first)
+            if constexpr (C::VREG) store_values();
             read_words();
+            if (begin + wave + NW < end) {
+                load_records(begin + wave + NW, page_of(begin + wave + NW));
+                if constexpr (C::VREG) load_values(begin + wave + NW, page_of(begin + wave + NW));
+            }
+            if constexpr (!C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
         for (int step = begin + wave; step < end; step += NW) {
             const bool more = step + NW < end, two_more = step + 2 * NW < end;
@@ -463,34 +481,48 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 const float rho = __uint_as_float(e.w);
                 return half_triplet(rho * __uint_as_float(e.x), rho * __uint_as_float(e.y), rho * __uint_as_float(e.z));
             };
-            uint4 ent[2][2];
+            // (one row block: both key blocks at once, as a product that adds to the last one's result waits for it)
+            constexpr int NB = LIVE == 1 ? 2 : 1, NS = 2 * KS / NB;
+            uint4 ent[2][NB][2];
             auto ask = [&](auto s_) __attribute__((always_inline)) {
-                constexpr int s = decltype(s_)::value, kb = s / KS, kk = s % KS;
-                ent[s % 2][0] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk>{});
-                ent[s % 2][1] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk + 1>{});
+                constexpr int s = decltype(s_)::value, kk = s % KS;
+                static_for<0, NB>([&](auto b_) {
+                    constexpr int kb = decltype(b_)::value + s / KS;
+                    ent[s % 2][decltype(b_)::value][0] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk>{});
+                    ent[s % 2][decltype(b_)::value][1] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk + 1>{});
+                });
             };
             ask(std::integral_constant<int, 0>{});
-            static_for<0, 2 * KS>([&](auto s_) {
-                constexpr int s = decltype(s_)::value, kb = s / KS, kk = s % KS;
-                if constexpr (s + 1 < 2 * KS) {
+            static_for<0, NS>([&](auto s_) {
+                constexpr int s = decltype(s_)::value, kk = s % KS;
+                if constexpr (s + 1 < NS) {
                     ask(std::integral_constant<int, s + 1>{});
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) gamma[e / 4][e % 4] = *reinterpret_cast<const float *>(stage + ((e / 4) * 16 + 4 * g + e % 4) * C::RST);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                // two entries (leading parts, remainders) to two operands: the halves in the middle change places
-                uint4 a = triplet(ent[s % 2][0]), b = triplet(ent[s % 2][1]);
-                asm("v_swap_b32 %0, %1" : "+v"(a.z), "+v"(b.x));
-                asm("v_swap_b32 %0, %1" : "+v"(a.w), "+v"(b.y));
-                const half8_t kh = __builtin_bit_cast(half8_t, a), kl = __builtin_bit_cast(half8_t, b);
+                half8_t kh[NB], kl[NB];
 #pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb)
-                    score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[rb][kk], kk == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : score[kb][rb], 0, 0, 0);
+                for (int b = 0; b < NB; ++b) {
+                    // two entries (leading parts, remainders) to two operands: the halves in the middle change places
+                    uint4 x = triplet(ent[s % 2][b][0]), y = triplet(ent[s % 2][b][1]);
+                    asm("v_swap_b32 %0, %1" : "+v"(x.z), "+v"(y.x));
+                    asm("v_swap_b32 %0, %1" : "+v"(x.w), "+v"(y.y));
+                    kh[b] = __builtin_bit_cast(half8_t, x);
+                    kl[b] = __builtin_bit_cast(half8_t, y);
+                }
+                // (each of these loops has products that do not wait for each other)
+                constexpr int first = s / KS;
 #pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[rb][kk], score[kb][rb], 0, 0, 0);
+                for (int e = 0; e < NB * LIVE; ++e)
+                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], qh[e % LIVE][kk], kk == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : score[first + e / LIVE][e % LIVE], 0, 0, 0);
 #pragma unroll
-                for (int rb = 0; rb < LIVE; ++rb) score[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[rb][kk], score[kb][rb], 0, 0, 0);
+                for (int e = 0; e < NB * LIVE; ++e)
+                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], ql[e % LIVE][kk], score[first + e / LIVE][e % LIVE], 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < NB * LIVE; ++e)
+                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl[e / LIVE], qh[e % LIVE][kk], score[first + e / LIVE][e % LIVE], 0, 0, 0);
             });
 #pragma unroll
             for (int rb = 0; rb < LIVE; ++rb)
@@ -538,11 +570,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             // The values have arrived; the records of the step after the next are asked for only now, as waiting for what a load
             // wrote to LDS waits for every load. Rows past the last token are made zeros: their probabilities are zero, but what
             // lies there may be no number.
-            wait_loads<0>();
-            if (two_more) {
-                if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
-                load_records(step + 2 * NW, page_of(step + 2 * NW));
-            }
+            if constexpr (!C::VREG) wait_loads<0>();
             const int last = len - 1 - step * kPrefixKeys;
             if (last < kPrefixKeys - 1) {
 #pragma unroll
@@ -591,7 +619,20 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_lo[rb], oacc[rb][cb], 0, 0, 0);
             }
             wait_lds();                  // (the reads are done before anything new is asked for in their place)
-            if (more) load_values(step + NW, page_of(step + NW));
+            if (more) {
+                if constexpr (C::VREG) {
+                    __builtin_amdgcn_wave_barrier();
+                    store_values();
+                    __builtin_amdgcn_wave_barrier();
+                }
+                // (the records first: they are waited for first, and a wait for them is not one for the values)
+                if (two_more) {
+                    if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
+                    load_records(step + 2 * NW, page_of(step + 2 * NW));
+                    if constexpr (C::VREG) load_values(step + 2 * NW, page_of(step + 2 * NW));
+                }
+                if constexpr (!C::VREG) load_values(step + NW, page_of(step + NW));
+            }
         }
 
         // ---- the wavefronts' results join ----
