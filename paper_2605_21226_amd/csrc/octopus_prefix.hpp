@@ -57,7 +57,7 @@ struct PrefixCfg {
     // between the instructions' pieces put four rows that follow each other on 32 different banks (the transposed reads take four).
     static constexpr int NVAL = D / 16;
     static constexpr int VST = 1024 + 32;
-    static constexpr bool VREG = D != 128;
+    static constexpr bool VREG = D == 256;
     static constexpr int VAL = NVAL * VST;                         // bytes of a step's values
     // Query operands in LDS: a row's leading parts and its remainders; rows 16 bytes apart beyond their size, so that the 16 rows read
     // at once lie on all banks.  The wavefronts' results: rows 16 bytes apart for the same reason.  Both take the values' place.
@@ -118,6 +118,10 @@ __device__ __forceinline__ void wait_lds() {
     __builtin_amdgcn_s_waitcnt(0xc07f);
     __asm__ volatile("" ::: "memory");
 }
+
+// The workgroup's barrier for what is in LDS. (__syncthreads waits for every load and store to memory as well: for the partial results on
+// their way out, whose acknowledgement takes 2000 clocks and more, and for the records and pages asked for ahead.)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <class P>
 __device__ __forceinline__ void build_prefix_tables(PrefixSmem<P> &sm, int tid) {
@@ -182,7 +186,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             if (lane < NR) sm.c_rho[wave][lane] = rho * (C::J0 ? 1.0f : kUnitScale);
         }
     }
-    __syncthreads();
+    lds_barrier();
     build_prefix_tables<P>(sm, threadIdx.x);
 
     unsigned char *stage = sm.rec[wave], *vals = place + wave * C::VAL;
@@ -306,7 +310,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             asked[p][0] = *reinterpret_cast<const u32x4a_t *>(src);
             asked[p][1] = *reinterpret_cast<const u32x4a_t *>(src + (shp.q_is_bf16 ? 0 : 16));
         }
-        __syncthreads();                 // tables complete; the last segment's results have been read
+        lds_barrier();                 // tables complete; the last segment's results have been read
 #pragma unroll
         for (int p = 0; p < C::QPASS; ++p) {
             const int local = tid / C::QLANES + p * C::QROWS;
@@ -358,7 +362,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 }
             }
         }
-        __syncthreads();
+        lds_barrier();
         auto walk = [&](auto live_) __attribute__((always_inline)) {
         constexpr int LIVE = decltype(live_)::value;   // blocks of 16 rows with rows
         half8_t qh[LIVE][KS], ql[LIVE][KS];
@@ -405,7 +409,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
         }
         all_see = __builtin_amdgcn_readfirstlane(all_see);
-        __syncthreads();                 // the operands have been read: the values' places are the wavefronts' own now
+        lds_barrier();                 // the operands have been read: the values' places are the wavefronts' own now
 
         // ---- the steps ----
         float m_ref[LIVE], l_run[LIVE];
@@ -645,7 +649,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 sm.ml[wave][rb * 16 + n][1] = l_run[rb];
             }
         }
-        __syncthreads();                 // (the staging areas are free from here on, too)
+        lds_barrier();                 // (the staging areas are free from here on, too)
         float *out = reinterpret_cast<float *>(place);   // [wavefront][16 rows][OST]
         const int64_t prow0 = shared ? static_cast<int64_t>(kvh) * all_rows * splits
                                      : shp.own_partials + (static_cast<int64_t>(seq) * shp.n_kv_heads + kvh) * own_rows * splits;
@@ -658,7 +662,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 *reinterpret_cast<f32x4_t *>(out + (wave * 16 + n) * C::OST + 16 * cb + 4 * g) = oacc[rb][cb] * weight;
-            __syncthreads();
+            lds_barrier();
             for (int e = tid; e < 16 * D / 4; e += C::NT) {
                 const int r = e / (D / 4), row = row0 + rb * 16 + r;
                 if (row >= rows) continue;
@@ -677,7 +681,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     part_ml[prow * 2 + 1] = l;
                 }
             }
-            __syncthreads();
+            lds_barrier();
         }
         };
         if (RB == 1 || live == 1) walk(std::integral_constant<int, 1>{});
