@@ -20,9 +20,12 @@ struct ReadSmem {
     float c_rho[P::NCLASS][kMaxLevels];
 };
 
+// (wavefronts a workgroup: at head dimension 256, whose tile in LDS lets two workgroups into a compute unit, twice as many)
+constexpr int read_waves(int d) { return d == 256 ? 8 : 4; }
+
 template <class P>
-__global__ __launch_bounds__(256) void read_tokens_kernel(DeviceBooks books, ReadCall a) {
-    constexpr int D = P::D, LPR = D / 8, RPP = 256 / LPR, NWV = 4;
+__global__ __launch_bounds__(read_waves(P::D) * 64) void read_tokens_kernel(DeviceBooks books, ReadCall a) {
+    constexpr int D = P::D, NWV = read_waves(D), NT = NWV * 64, LPR = D / 8, RPP = NT / LPR;
     __shared__ ReadSmem<P> sm;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -46,12 +49,12 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(DeviceBooks books, Rea
         }
         {   // a level per lane, of one array per wavefront
             typedef const float __attribute__((address_space(4))) *arg_t;
-            const float level = ((arg_t)__builtin_amdgcn_kernarg_segment_ptr())[offsetof(DeviceBooks, c_xi) / 4 + wave * kMaxLevels + lane];
-            if (wave % 2 < P::NCLASS) (wave < 2 ? sm.c_xi[wave % P::NCLASS] : sm.c_rho[wave % P::NCLASS])[lane] = level;
+            const float level = ((arg_t)__builtin_amdgcn_kernarg_segment_ptr())[offsetof(DeviceBooks, c_xi) / 4 + (wave % 4) * kMaxLevels + lane];
+            if (wave < 4 && wave % 2 < P::NCLASS) (wave < 2 ? sm.c_xi[wave % P::NCLASS] : sm.c_rho[wave % P::NCLASS])[lane] = level;
         }
         __syncthreads();
-        build_dir_lut<P::BD0>(sm.dir0, sm.c_xi[0], tid, 256);
-        if constexpr (P::NCLASS == 2) build_dir_lut<P::BD1>(sm.dir1, sm.c_xi[P::NCLASS - 1], tid, 256);
+        build_dir_lut<P::BD0>(sm.dir0, sm.c_xi[0], tid, NT);
+        if constexpr (P::NCLASS == 2) build_dir_lut<P::BD1>(sm.dir1, sm.c_xi[P::NCLASS - 1], tid, NT);
         __syncthreads();
         const float gamma = __uint_as_float(w[0]) * inv_sqrt_dim<D>();
         auto unpack = [&](auto wv_) __attribute__((always_inline)) {
@@ -65,12 +68,9 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(DeviceBooks books, Rea
                 sm.u[3 * i + 2][lane] = rho * n.z;
             });
         };
-        switch (wave) {
-            case 0: unpack(std::integral_constant<int, 0>{}); break;
-            case 1: unpack(std::integral_constant<int, 1>{}); break;
-            case 2: unpack(std::integral_constant<int, 2>{}); break;
-            default: unpack(std::integral_constant<int, 3>{}); break;
-        }
+        static_for<0, NWV>([&](auto wv_) {
+            if (wave == decltype(wv_)::value) unpack(wv_);
+        });
         __syncthreads();
         constexpr int R = D / 8;
         for (int low = wave; low < 8; low += NWV) {
@@ -96,23 +96,48 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(DeviceBooks books, Rea
         }
     }
     if (a.v_out != nullptr) {
-        for (int key = tid / LPR; key < kWave; key += RPP) {
-            const int64_t slot = tile * kWave + key;
-            if (slot < lo || slot >= hi) continue;
-            float x[8];
-            if (a.v_bits == 0) {
-                load_eight(a.v_pool, (slab * kWave + key) * D + col, 1, x);
-            } else {
-                // v^ = zero + scale code: channel j's code at bit v_bits j of the row, scale and zero of its group after the codes
-                const int row_bytes = a.v_bits * D / 8 + D / a.v_group * 8;
-                const unsigned char *row = static_cast<const unsigned char *>(a.v_pool) + (slab * kWave + key) * row_bytes;
-                uint32_t codes = 0u;
-                for (int b = 0; b < a.v_bits; ++b) codes |= static_cast<uint32_t>(row[col / 8 * a.v_bits + b]) << (8 * b);
-                const float2 meta = *reinterpret_cast<const float2 *>(row + a.v_bits * D / 8 + col / a.v_group * 8);
+        constexpr int KEYS = kWave / RPP;        // rows a thread reads eight channels of: all of them asked for, then written
+        const int first = static_cast<int>(lo - tile * kWave), last = static_cast<int>(hi - 1 - tile * kWave);
+        auto write = [&](int key, const float (&x)[8]) __attribute__((always_inline)) {
+            if (key >= first && key <= last)
+                store_eight(a.v_out, ((static_cast<int64_t>(seq) * a.n_tok + tile * kWave + key - start) * a.n_kv_heads + kvh) * D + col, a.out_is_bf16, x);
+        };
+        float x[8];
+        if (a.v_bits == 0) {
+            uint4 row[KEYS];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = fmaf(meta.x, static_cast<float>((codes >> (a.v_bits * e)) & ((1u << a.v_bits) - 1u)), meta.y);
+            for (int i = 0; i < KEYS; ++i) {
+                const int key = min(max(tid / LPR + i * RPP, first), last);
+                row[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.v_pool) + (slab * kWave + key) * D + col);
             }
-            store_eight(a.v_out, ((static_cast<int64_t>(seq) * a.n_tok + slot - start) * a.n_kv_heads + kvh) * D + col, a.out_is_bf16, x);
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const uint32_t two[4] = {row[i].x, row[i].y, row[i].z, row[i].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = __uint_as_float((e & 1) ? two[e / 2] & 0xffff0000u : two[e / 2] << 16);
+                write(tid / LPR + i * RPP, x);
+            }
+        } else {
+            // v^ = zero + scale code: channel j's code at bit v_bits j of the row, scale and zero of its group after the codes (so that
+            // four bytes from any code's are the row's)
+            typedef uint32_t word_t __attribute__((aligned(1)));
+            const int code_bytes = a.v_bits * D / 8, row_bytes = code_bytes + D / a.v_group * 8;
+            uint32_t codes[KEYS];
+            float2 meta[KEYS];
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const int key = min(max(tid / LPR + i * RPP, first), last);
+                const unsigned char *row = static_cast<const unsigned char *>(a.v_pool) + (slab * kWave + key) * row_bytes;
+                codes[i] = *reinterpret_cast<const word_t *>(row + col / 8 * a.v_bits);
+                meta[i] = *reinterpret_cast<const float2 *>(row + code_bytes + col / a.v_group * 8);
+            }
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[e] = fmaf(meta[i].x, static_cast<float>((codes[i] >> (a.v_bits * e)) & ((1u << a.v_bits) - 1u)), meta[i].y);
+                write(tid / LPR + i * RPP, x);
+            }
         }
     }
 }
@@ -120,7 +145,7 @@ __global__ __launch_bounds__(256) void read_tokens_kernel(DeviceBooks books, Rea
 template <class P>
 int launch_read_plan(const octopus_codebooks_t &cb, const ReadCall &a, hipStream_t stream) {
     const int tiles = (a.n_tok + kWave - 1) / kWave + (a.start_pos ? 1 : 0);
-    hipLaunchKernelGGL(read_tokens_kernel<P>, dim3(tiles, a.n_kv_heads, a.n_seq), dim3(256), 0, stream, device_books(cb), a);
+    hipLaunchKernelGGL(read_tokens_kernel<P>, dim3(tiles, a.n_kv_heads, a.n_seq), dim3(read_waves(P::D) * 64), 0, stream, device_books(cb), a);
     return static_cast<int>(hipGetLastError());
 }
 
