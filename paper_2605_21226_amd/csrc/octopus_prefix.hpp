@@ -160,7 +160,9 @@ struct QuarterStream {
     static constexpr int READ = ALIGNED ? WORDS : WORDS + 1;
 };
 
-template <class P>
+// CAUSAL: rows of a sequence may see fewer of its tokens than others.  (A kernel of its own: what it takes to keep values that are no
+// numbers from the rows that do not see them costs the other one 4 to 10 % in registers.)
+template <class P, bool CAUSAL>
 __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_eu(PrefixCfg<P>::NW / 4))) void prefix_attention_kernel(
     DeviceBooks books, PrefixShape shp, const unsigned char *__restrict__ k_pool, const unsigned char *__restrict__ v_pool,
     const int32_t *__restrict__ prefix_table, const int32_t *__restrict__ prefix_len, const int32_t *__restrict__ block_table,
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             factor[rb] = sm.factor[rb * 16 + n];
             limit[rb] = len;
             const int row = row0 + rb * 16 + n;
-            if (!shared && shp.causal && row < rows) {
+            if (CAUSAL && !shared && row < rows) {
                 const int nq = q_lens != nullptr ? min(max(q_lens[seq], 0), shp.n_q) : shp.n_q;
                 limit[rb] = min(max(len - nq + row / hpk + 1, 0), len);
                 all_see = min(max(len - nq + row0 / hpk + 1, 0), len);
@@ -583,6 +585,46 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                         *reinterpret_cast<uint4 *>(vals + e * C::VST + lane * 16) = make_uint4(0u, 0u, 0u, 0u);
                 __builtin_amdgcn_wave_barrier();
             }
+            // A value that is no finite number makes its channel NaN for the rows that see its token, and a zero for the others: what
+            // they do not see would reach them through the product otherwise.
+            if (CAUSAL && min((step + 1) * kPrefixKeys, len) > all_see) {
+                auto none = [](uint32_t two, int j) { return (two >> (16 * j) & 0x7f80u) == 0x7f80u; };
+                uint32_t odd = 0;                // keys that have such a value
+#pragma unroll
+                for (int e = 0; e < C::NVAL; ++e) {
+                    const uint4 piece = *reinterpret_cast<const uint4 *>(vals + e * C::VST + lane * 16);
+                    const uint32_t two[4] = {piece.x, piece.y, piece.z, piece.w};
+                    bool any = false;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) any = any || none(two[j / 2], j % 2);
+                    const uint64_t lanes = __ballot(any);
+#pragma unroll
+                    for (int part = 0; part < kWave / LPR; ++part)
+                        if ((lanes >> (part * LPR) & ((1ull << (LPR - 1)) * 2 - 1)) != 0) odd |= 1u << (part * C::NVAL + e);
+                }
+                if (odd != 0) {
+                    for (uint32_t left = odd; left != 0; left &= left - 1) {
+                        const int key = __ffs(static_cast<int>(left)) - 1;
+                        const unsigned char *row = vals + (key % C::NVAL) * C::VST + (key / C::NVAL) * (2 * D) + 8 * g;
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb) {
+                            const uint2 four = *reinterpret_cast<const uint2 *>(row + 32 * cb);
+#pragma unroll
+                            for (int rb = 0; rb < LIVE; ++rb)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (none(j < 2 ? four.x : four.y, j % 2) && step * kPrefixKeys + key < limit[rb]) oacc[rb][cb][j] = NAN;
+                        }
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                    for (int e = 0; e < C::NVAL; ++e) {
+                        uint16_t *piece = reinterpret_cast<uint16_t *>(vals + e * C::VST + lane * 16);
+                        for (int j = 0; j < 8; ++j)
+                            if (none(piece[j], 0)) piece[j] = 0;
+                    }
+                    __builtin_amdgcn_wave_barrier();
+                }
+            }
             // O^T += V^T P^T: k-slots 8 g .. + 3 are keys 4 g .. + 3 of the first block, the next four those of the second
             constexpr int AHEAD_V = 3;                   // (channels of this and the next two products are held)
             typedef __attribute__((address_space(3))) s16x4_t *tr_t;
@@ -696,9 +738,12 @@ int launch_prefix_plan(const octopus_codebooks_t &cb, const PrefixShape &s, cons
                        float *part_acc, hipStream_t stream) {
     const DeviceBooks books = device_books(cb);
     const int grid = s.n_segments < 256 ? s.n_segments : 256;
-    hipLaunchKernelGGL(prefix_attention_kernel<P>, dim3(grid), dim3(PrefixCfg<P>::NT), 0, stream, books, s,
-                       static_cast<const unsigned char *>(k_pool), static_cast<const unsigned char *>(v_pool), prefix_table, prefix_len,
-                       block_table, seq_lens, q_lens, part_ml, part_acc);
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(PrefixCfg<P>::NT), 0, stream, books, s, static_cast<const unsigned char *>(k_pool),
+                           static_cast<const unsigned char *>(v_pool), prefix_table, prefix_len, block_table, seq_lens, q_lens, part_ml, part_acc);
+    };
+    if (s.causal) go(prefix_attention_kernel<P, true>);
+    else go(prefix_attention_kernel<P, false>);
     return static_cast<int>(hipGetLastError());
 }
 
