@@ -15,6 +15,9 @@
  *   octopus_encode_values_paged, octopus_attn_decode_paged_vq,
  *   octopus_encode_qjl_paged, octopus_attn_decode_paged_qjl
  *                                                  the same codec and attention over a paged cache
+ *   octopus_append_paged, octopus_read_paged       a step's keys, values and queries, rotated by position, into pages;
+ *                                                  tokens of pages as values again
+ *   octopus_attn_decode_paged_prefix               attention of sequences that share a prefix
  *
  * Conventions
  *   - Plain C.  Every function returns 0 (OCTOPUS_OK) or a negative error
@@ -576,8 +579,8 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
  *                block_table and seq_lens are not looked at.
  *   out          device fp32 [n_seq][n_q][n_q_heads][d]; a query that sees no token yields zeros.
  *   workspace    device, 256-byte aligned, at least octopus_attn_prefix_workspace(...) bytes of the same shape; contents are scratch.
- * Values: a token that a query does not see for causality is a token of the sequence all the same, and one whose value is not a
- * finite number makes outputs of its step's queries NaN; tokens past the lengths are never looked at.
+ * A value that is not a finite number makes its channel no finite number either for the queries that see its token; what a query does
+ * not see (tokens past the lengths, later ones for causality) has no say, whatever it is.
  * Any n_q, n_seq and head ratio (all n_seq * n_q * n_q_heads <= 2^26 rows, n_seq * n_q <= 2^24).  octopus_profile_events takes the call.
  * Errors: EINVAL, EUNSUPPORTED (a plan or type without a kernel; the App. D pairs have none), EWORKSPACE, EHIP. */
 size_t octopus_attn_prefix_workspace(const octopus_codebooks_t *cb, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,
@@ -603,7 +606,7 @@ const char *octopus_strerror(int code);
 
 /* ---- measurement aids (not part of the method; nothing above depends on them) ----
  * octopus_profile_events: the next decode-attention call made by this thread (octopus_attn_decode, its _static,
- * _qjl, _vq and _hybrid forms, octopus_attn_decode_paged and its _hybrid, _vq and _qjl forms) records the HIP events `before` and `after` (hipEvent_t
+ * _qjl, _vq and _hybrid forms, octopus_attn_decode_paged and its _hybrid, _vq, _qjl and _prefix forms) records the HIP events `before` and `after` (hipEvent_t
  * passed as void*, caller-owned, created with timing enabled) on the call's stream immediately before and after
  * the launch of its fused decode kernel, i.e. around Alg. 2 proper without the split merge.  The query rotation is
  * inside where that kernel does it itself: at every bit width where a call of 32 or more query rows per KV head goes to the kernel

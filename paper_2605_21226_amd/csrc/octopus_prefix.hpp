@@ -349,7 +349,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             static_for<0, C::log2i(C::QLANES)>([&](auto bb) { top = fmaxf(top, lane_xor<(1 << decltype(bb)::value)>(top, lane)); });
             const int ex = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
             if (C::ROWS % C::QROWS == 0 || local < C::ROWS) {
-                if (qc == 0) sm.factor[local] = ldexpf(norm, ex);
+                // (not zero, which a scale of zero would make it: what a row does not see has a score of minus infinity, and stays there)
+                if (qc == 0) sm.factor[local] = fmaxf(ldexpf(norm, ex), 1.17549435e-38f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int c = 8 * qc + e, t = c / 3;

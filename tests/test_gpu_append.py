@@ -260,3 +260,56 @@ def test_read_ranges_and_what_is_left_alone(n_tok, start, lens):
     check_read(a, n_tok, start, lens, k, None)
     _, v = read(a, n_tok, start, lens, keys=False, dtype=torch.bfloat16)
     check_read(a, n_tok, start, lens, None, v)
+
+
+def test_nothing_to_append_or_read():
+    s = Setup(128, 3, 2, 2, 2, 4, [3, 60])
+    empty = s.k_dev[:, :0].contiguous()
+    binding.octopus_append_paged(s.cb, empty, empty, s.signs_dev, s.k_pool, s.v_pool.view(torch.bfloat16), s.n_pages, s.block_dev, start_pos=s.start_dev)
+    s.append(new_lens=ints([0, -3]))
+    assert bool((s.k_pool == FILL).all()) and bool((s.v_pool == FILL).all()) and bool((s.q_out == 7.0).all())
+    out = torch.full((2, 4, 2, 128), 5.0, device=DEV)
+    binding.octopus_read_paged(s.cb, s.signs_dev, s.k_pool, s.v_pool.view(torch.bfloat16), s.n_pages, s.block_dev, out[:, :0].contiguous(), None)
+    binding.octopus_read_paged(s.cb, s.signs_dev, s.k_pool, s.v_pool.view(torch.bfloat16), s.n_pages, s.block_dev, out, out.clone(), lens=ints([0, -1]))
+    torch.cuda.synchronize()
+    assert bool((out == 5.0).all())
+
+
+@pytest.mark.parametrize("n_new", [1, 70])
+def test_page_ids_outside_the_pool_are_clamped(n_new):
+    a, b = (Setup(128, 3, 2, 2, 2, n_new, [3, 60], pages=3, seed=1) for _ in range(2))
+    for s, ids in ((a, (0, a.n_pages - 1)), (b, (-2 ** 31, 2 ** 31 - 1))):
+        s.block[:] = np.asarray([[3, 4, ids[0]], [5, 6, ids[1]]])[:, ::-1]
+        s.block_dev = ints(s.block)
+        s.append()
+    assert torch.equal(a.k_pool, b.k_pool) and torch.equal(a.v_pool, b.v_pool) and torch.equal(a.q_out, b.q_out)
+    out = [torch.zeros((2, n_new, 2, 128), device=DEV) for _ in range(4)]
+    for s, k, v in ((a, *out[:2]), (b, *out[2:])):
+        binding.octopus_read_paged(s.cb, s.signs_dev, s.k_pool, s.v_pool.view(torch.bfloat16), s.n_pages, s.block_dev, k, v, start_pos=s.start_dev)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3]) and float(out[0].abs().sum()) > 0
+
+
+@pytest.mark.parametrize("n_new", [1, 130])
+def test_keys_that_are_no_numbers_are_encoded_as_by_the_separate_call(n_new):
+    s = Setup(128, 3, 2, 2, 2, n_new, [5, 64], rot=0)
+    s.k_dev[0, 0, 0, 3], s.k_dev[1, n_new - 1, 1, 100], s.k_dev[1, 0, 0] = float("nan"), float("inf"), 0.0
+    pool = torch.full_like(s.k_pool, FILL)
+    binding.octopus_encode_paged(s.cb, s.k_dev.contiguous(), s.signs_dev, pool, s.n_pages, s.block_dev, s.start_dev)
+    s.append()
+    assert torch.equal(s.k_pool, pool)
+
+
+def test_appending_on_another_stream():
+    s, t = (Setup(128, 3, 2, 2, 2, 200, [5, 64], seed=2) for _ in range(2))
+    s.append()
+    stream, kept = torch.cuda.Stream(), t.qkv.clone()
+    t.qkv.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        big = torch.ones(4096, 4096, device=DEV)
+        for _ in range(4):
+            big = big @ big * 1e-4
+        t.qkv.copy_(kept)
+        t.append(stream=stream)
+    assert torch.equal(s.k_pool, t.k_pool) and torch.equal(s.v_pool, t.v_pool) and torch.equal(s.q_out, t.q_out)

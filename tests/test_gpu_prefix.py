@@ -183,3 +183,109 @@ def test_one_table_for_prefix_and_own_pages_agrees_with_the_paged_call():
     torch.cuda.synchronize()
     got = b.call()
     assert torch.allclose(got, out, rtol=0, atol=2e-4 * float(out.abs().max()))   # (2^-13 of the row-group kernel's bf16 pairs)
+
+
+@pytest.mark.parametrize("d,bits", [(64, 4), (128, 3), (128, 1.5), (256, 2.5)])
+def test_tokens_a_query_does_not_see_have_no_say_whatever_they_are(d, bits):
+    """Causal queries over own tokens whose last ones have values and keys that are no numbers: the queries that do not see them give
+    the bits that they give with zeros there; of a value's channel that is none, those that do give none."""
+    b = Batch(d, bits, 6, 2, 9, 40, [9, 70, 33], seed=d + 3)
+    b.v_pool[b.v_pool.isnan()] = 0.0
+    clean = b.call(causal=True)
+    token = [5, 66, 30]                                     # of 9, 70 and 33: seen by the queries from 5, 5 and 6 on
+    first = [5, 5, 6]
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        v = b.v_pool.clone()
+        for s, t in enumerate(token):
+            v[b.table[s][t // 64], :, t % 64, 1::7] = bad
+        b.v_pool, v = v, b.v_pool
+        out = b.call(causal=True)
+        b.v_pool = v
+        for s in range(3):
+            assert torch.equal(out[s, :first[s]], clean[s, :first[s]])
+            hit = ~torch.isfinite(out[s, first[s]:])
+            assert bool(hit[..., 1::7].all()) and int(hit.sum()) == hit[..., 1::7].numel()
+    kp = b.k_pool.clone()
+    for s, t in enumerate(token):                           # a norm that is no number, in the first four bytes of the record
+        kp.view(b.n_pages, b.n_kv, -1, 64, 16)[int(b.table[s][t // 64]), :, 0, t % 64, :4] = 0xFF
+    b.k_pool = kp
+    out = b.call(causal=True)
+    for s in range(3):
+        assert torch.equal(out[s, :first[s]], clean[s, :first[s]]) and bool(out[s, first[s]:].isnan().all())
+
+
+def test_values_that_are_no_numbers_stay_in_their_channel_and_sequence():
+    b = Batch(128, 3, 8, 2, 1, 100, [50, 30], seed=14)
+    clean = b.call()
+    b.v_pool[int(b.table[0][0]), 1, 20, 5] = float("inf")
+    out = b.call()
+    assert torch.equal(out[1], clean[1]) and torch.equal(out[0, :, :4], clean[0, :, :4])      # (KV head 1 has query heads 4 .. 7)
+    hit = ~torch.isfinite(out[0, :, 4:])
+    assert bool(hit[..., 5].all()) and int(hit.sum()) == hit[..., 5].numel()
+
+
+def test_garbage_in_queries_that_do_not_count():
+    b = Batch(64, 3, 4, 2, 5, 60, [20, 40, 8], seed=8)
+    q_lens = [5, 2, 0]
+    want = b.call(q_lens=q_lens, causal=True)
+    for s, n in enumerate(q_lens):
+        b.q_dev[s, n:] = float("nan")
+    assert torch.equal(b.call(q_lens=q_lens, causal=True), want)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_no_tokens_at_all(causal):
+    b = Batch(128, 3, 8, 2, 2, 70, [30, 40], seed=3)
+    assert bool((b.call(max_prefix=0, max_len=0, causal=causal) == 0).all())          # neither table is looked at
+    b.prefix, b.lens = 0, [0, 0]
+    assert bool((b.call(max_prefix=70, max_len=40, causal=causal) == 0).all())        # bounds of the host, lengths of the device
+    b.prefix, b.lens = -5, [-1, -2 ** 31]
+    assert bool((b.call(max_prefix=70, max_len=40, causal=causal) == 0).all())
+
+
+def test_lengths_and_pages_outside_their_bounds_are_clamped():
+    b = Batch(128, 3, 8, 2, 1, 128, [64, 64], seed=4, slack=0, spare=0)
+    want = b.call()
+    b.prefix, b.lens = 2 ** 31 - 1, [1000, 2 ** 31 - 1]
+    assert torch.equal(b.call(max_prefix=128, max_len=64), want)
+    b = Batch(128, 3, 8, 2, 1, 64, [64, 64], seed=4, slack=0, spare=0)
+    b.prefix_table[0], b.table[0][0], b.table[1][0] = 0, b.n_pages - 1, 0
+    want = b.call()
+    b.prefix_table[0], b.table[0][0], b.table[1][0] = -7, 2 ** 31 - 1, -2 ** 31
+    assert torch.equal(b.call(), want)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.4, 3.0])
+def test_scales(scale):
+    b = Batch(128, 2, 4, 2, 1, 50, [40, 3], seed=6)
+    b.scale = scale
+    b.check(b.call())
+
+
+def test_another_stream():
+    """The call waits for what is on the stream that it is given, and for nothing else."""
+    b = Batch(128, 3, 8, 2, 1, 900, [200, 100], seed=12)
+    want = b.call()
+    q, stream = b.q_dev.clone(), torch.cuda.Stream()
+    for _ in range(3):
+        b.q_dev.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            big = torch.ones(4096, 4096, device=DEV)
+            for _ in range(4):
+                big = big @ big * 1e-4                       # the stream has something to do first
+            b.q_dev.copy_(q)
+            assert torch.equal(b.call(stream=stream), want)
+
+
+def test_profile_events_enclose_the_attention():
+    b = Batch(128, 3, 8, 2, 1, 4000, [200, 100], seed=13)
+    want = b.call()
+    before, after = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    before.record(), after.record()
+    torch.cuda.synchronize()
+    binding.octopus_profile_events(before, after)
+    assert torch.equal(b.call(), want)
+    assert 0.0 < before.elapsed_time(after) < 1000.0
+    first = before.elapsed_time(after)
+    assert torch.equal(b.call(), want) and before.elapsed_time(after) == first       # one call only
