@@ -36,11 +36,11 @@ struct PrefixCfg {
     static constexpr int RB = prefix_rows(D) / 16;
     static constexpr int ROWS = 16 * RB;
     static constexpr int NT = kWave * NW;
-    // triplets of each class that a lane group decodes; one class: padded to whole operands
-    static constexpr int T0 = P::NCLASS == 1 ? ((P::NTRI + 7) / 8) * 2 : (P::NT0 + 3) / 4;
+    // triplets of each class that a lane group decodes
+    static constexpr int T0 = ((P::NCLASS == 1 ? P::NTRI : P::NT0) + 3) / 4;
     static constexpr int T1 = P::NCLASS == 2 ? (P::NT1 + 3) / 4 : 0;
     static constexpr int TPL = T0 + T1;
-    static constexpr int KS = (TPL + 1) / 2;                       // operands (of two triplets) a key
+    static constexpr int KS = (3 * TPL + 7) / 8;                   // operands of a key: eight coordinates each, a lane group's one after the other
     static constexpr bool J0 = joint_codes(P::BD0, P::BN0);
     static constexpr bool J1 = P::NCLASS == 2 && joint_codes(P::BD1, P::BN1);
     static_assert(P::NCLASS == 1 || (J0 && J1), "two classes have joint tables");
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     const bool second = P::NCLASS == 2 && t >= P::NT0;
                     const int of = second ? t - P::NT0 : t, each = second ? (C::T1 > 0 ? C::T1 : 1) : C::T0;
                     const int at = of % each + (second ? C::T0 : 0);
-                    unsigned char *to = place + local * C::QST + ((of / each) * KS + at / 2) * 16 + ((at % 2) * 4 + c % 3) * 2;
+                    unsigned char *to = place + local * C::QST + (of / each) * (KS * 16) + (3 * at + c % 3) * 2;
                     const float y = ldexpf(x[e], -ex);
                     const _Float16 hi = static_cast<_Float16>(y), lo = static_cast<_Float16>(y - static_cast<float>(hi));
                     *reinterpret_cast<_Float16 *>(to) = hi;
@@ -374,31 +374,35 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         int all_see = len;               // tokens that every row sees
 #pragma unroll
         for (int rb = 0; rb < LIVE; ++rb) {
-            // (places that no coordinate has: every fourth, those of triplets past a class's last and of coordinates past the last; what
-            // lies there is left over)
+            // (places that no coordinate has: those of triplets past a class's last, of coordinates past the last and behind a lane
+            // group's triplets; what lies there is left over)
             const unsigned char *from = place + (rb * 16 + n) * C::QST + g * (KS * 16);
             static_for<0, KS>([&](auto kk_) {
                 constexpr int kk = decltype(kk_)::value;
                 uint4 h = *reinterpret_cast<const uint4 *>(from + kk * 16), l = *reinterpret_cast<const uint4 *>(from + 4 * KS * 16 + kk * 16);
-                auto keep = [&](auto at_, uint32_t &first, uint32_t &second) __attribute__((always_inline)) {
-                    constexpr int at = decltype(at_)::value;
-                    constexpr bool two = P::NCLASS == 2 && at >= C::T0;
-                    constexpr int each = two ? C::T1 : C::T0, count = two ? P::NT1 : P::NT0, within = two ? at - C::T0 : at;
-                    constexpr int base = two ? P::NT0 : 0;
-                    second &= 0xffffu;
-                    if constexpr (at >= C::TPL) {
-                        first = second = 0u;
-                    } else if constexpr (3 * each + within >= count - 1) {   // (some lane groups have none, or the last)
-                        const int t = g * each + within, left = t < count ? D - 3 * (base + t) : 0;   // coordinates of the triplet
-                        if (left < 3) second = 0u;
-                        if (left < 2) first &= 0xffffu;
-                        if (left < 1) first = 0u;
-                    }
+                auto keep = [&](auto at_, uint32_t &hi, uint32_t &lo) __attribute__((always_inline)) {
+                    static_for<0, 2>([&](auto half_) {
+                        constexpr int place = decltype(at_)::value + decltype(half_)::value, at = place / 3;
+                        constexpr uint32_t others = decltype(half_)::value ? 0xffffu : 0xffff0000u;
+                        constexpr bool two = P::NCLASS == 2 && at >= C::T0;
+                        constexpr int each = two ? C::T1 : C::T0, count = two ? P::NT1 : P::NT0, within = two ? at - C::T0 : at;
+                        constexpr int base = two ? P::NT0 : 0;
+                        if constexpr (at >= C::TPL) {
+                            hi &= others;
+                            lo &= others;
+                        } else if constexpr (3 * each + within >= count - 1) {   // (some lane groups have none, or the last)
+                            const int t = g * each + within;
+                            if (t >= count || place % 3 >= D - 3 * (base + t)) {
+                                hi &= others;
+                                lo &= others;
+                            }
+                        }
+                    });
                 };
-                keep(std::integral_constant<int, 2 * kk>{}, h.x, h.y);
-                keep(std::integral_constant<int, 2 * kk + 1>{}, h.z, h.w);
-                keep(std::integral_constant<int, 2 * kk>{}, l.x, l.y);
-                keep(std::integral_constant<int, 2 * kk + 1>{}, l.z, l.w);
+                keep(std::integral_constant<int, 8 * kk>{}, h.x, l.x);
+                keep(std::integral_constant<int, 8 * kk + 2>{}, h.y, l.y);
+                keep(std::integral_constant<int, 8 * kk + 4>{}, h.z, l.z);
+                keep(std::integral_constant<int, 8 * kk + 6>{}, h.w, l.w);
                 qh[rb][kk] = __builtin_bit_cast(half8_t, h);
                 ql[rb][kk] = __builtin_bit_cast(half8_t, l);
             });
@@ -453,13 +457,11 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             const bool more = step + NW < end, two_more = step + 2 * NW < end;
             f32x4_t score[2][LIVE];      // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
             float gamma[2][4];
-            // An operand (two triplets) of a key block at a time; the entries of the next one are asked for before the products of this
-            // one, as LDS takes longer to answer than a product.
+            // An operand of a key block at a time; the entries of the next one (triplets that begin there) are asked for before the
+            // products of this one, as LDS takes longer to answer than a product.
             auto entry = [&](auto kb_, auto at_) __attribute__((always_inline)) -> uint4 {
                 constexpr int kb = decltype(kb_)::value, at = decltype(at_)::value;
-                if constexpr (at >= C::TPL) {
-                    return make_uint4(0u, 0u, 0u, 0u);
-                } else if constexpr (at < C::T0) {
+                if constexpr (at < C::T0) {
                     const uint32_t nrm = field_clamped<at * P::BN0, P::BN0>(wn0[kb]);
                     if constexpr (C::J0 && 2 * P::BD0 == 8 && C::R0 * 16 << P::BN0 == 256) {
                         // the code is a whole byte and the entry's offset has it as its second byte, above norm code and copy
@@ -490,14 +492,28 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             };
             // (one row block: both key blocks at once, as a product that adds to the last one's result waits for it)
             constexpr int NB = LIVE == 1 ? 2 : 1, NS = 2 * KS / NB;
-            uint4 ent[2][NB][2];
+            uint4 ent[2][C::TPL];            // (unrolled: an entry lives from being asked for to the operand that it ends in)
+            auto starts = [](int kk) constexpr { return (8 * kk + 2) / 3 < C::TPL ? (8 * kk + 2) / 3 : C::TPL; };
             auto ask = [&](auto s_) __attribute__((always_inline)) {
                 constexpr int s = decltype(s_)::value, kk = s % KS;
                 static_for<0, NB>([&](auto b_) {
                     constexpr int kb = decltype(b_)::value + s / KS;
-                    ent[s % 2][decltype(b_)::value][0] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk>{});
-                    ent[s % 2][decltype(b_)::value][1] = entry(std::integral_constant<int, kb>{}, std::integral_constant<int, 2 * kk + 1>{});
+                    static_for<starts(kk), starts(kk + 1)>([&](auto at_) { ent[kb][decltype(at_)::value] = entry(std::integral_constant<int, kb>{}, at_); });
                 });
+            };
+            // halves 2 w and 2 w + 1 of a lane group's coordinates of a key: of the leading parts or of the remainders
+            auto word = [&](auto kb_, auto w_, auto low_) __attribute__((always_inline)) -> uint32_t {
+                constexpr int kb = decltype(kb_)::value, at = 2 * decltype(w_)::value / 3, c = 2 * decltype(w_)::value % 3;
+                constexpr bool low = decltype(low_)::value;
+                if constexpr (at >= C::TPL) {
+                    return 0u;
+                } else {
+                    const uint32_t xy = low ? ent[kb][at].z : ent[kb][at].x, z = low ? ent[kb][at].w : ent[kb][at].y;
+                    if constexpr (c == 0) return xy;
+                    else if constexpr (c == 1) return __builtin_amdgcn_alignbit(z, xy, 16);
+                    else if constexpr (at + 1 >= C::TPL) return z;
+                    else return __builtin_amdgcn_perm(low ? ent[kb][at + 1].z : ent[kb][at + 1].x, z, 0x05040100u);
+                }
             };
             ask(std::integral_constant<int, 0>{});
             static_for<0, NS>([&](auto s_) {
@@ -510,15 +526,17 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 half8_t kh[NB], kl[NB];
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    // two entries (leading parts, remainders) to two operands: the halves in the middle change places
-                    uint4 x = triplet(ent[s % 2][b][0]), y = triplet(ent[s % 2][b][1]);
-                    asm("v_swap_b32 %0, %1" : "+v"(x.z), "+v"(y.x));
-                    asm("v_swap_b32 %0, %1" : "+v"(x.w), "+v"(y.y));
-                    kh[b] = __builtin_bit_cast(half8_t, x);
-                    kl[b] = __builtin_bit_cast(half8_t, y);
-                }
+                static_for<0, NB>([&](auto b_) {
+                    constexpr int b = decltype(b_)::value, kb = b + s / KS;
+                    static_for<starts(kk), starts(kk + 1)>([&](auto at_) { ent[kb][decltype(at_)::value] = triplet(ent[kb][decltype(at_)::value]); });
+                    auto four = [&](auto low_) __attribute__((always_inline)) {
+                        using K = std::integral_constant<int, kb>;
+                        return make_uint4(word(K{}, std::integral_constant<int, 4 * kk>{}, low_), word(K{}, std::integral_constant<int, 4 * kk + 1>{}, low_),
+                                          word(K{}, std::integral_constant<int, 4 * kk + 2>{}, low_), word(K{}, std::integral_constant<int, 4 * kk + 3>{}, low_));
+                    };
+                    kh[b] = __builtin_bit_cast(half8_t, four(std::false_type{}));
+                    kl[b] = __builtin_bit_cast(half8_t, four(std::true_type{}));
+                });
                 // (each of these loops has products that do not wait for each other)
                 constexpr int first = s / KS;
 #pragma unroll
