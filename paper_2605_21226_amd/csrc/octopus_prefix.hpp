@@ -6,11 +6,20 @@
 // and a row's output is sum_t p_t v_t / sum_t p_t over the prefix's tokens and the own ones the row may see.
 //
 // Both products run on the matrix cores and a key is decoded straight into the operand registers: the dot product does not care in
-// which order its terms come, so the terms are laid out as the table of (direction, norm) codes holds them -- (x, y, z, 0) of a
-// triplet as four fp16 numbers and their four remainders, one 16-byte entry, half an operand of each.  A lane of group g = lane / 16
-// decodes the g-th quarter of the triplets of key lane % 16.  No decoded key is written anywhere, no barrier is in the loop: a
-// wavefront owns steps of 32 tokens (its records and value rows staged in LDS of its own) and 32 query rows, the wavefronts of a
-// workgroup take the steps of a segment in turn, and their (m, l, acc) join at its end.
+// which order its terms come, so a lane of group g = lane / 16 decodes the g-th quarter of the triplets of key lane % 16 and puts their
+// coordinates one after the other into the eight places that it has in each operand.  A table by (direction, norm) codes holds
+// (x, y, z, 0) of a triplet as four fp16 numbers and their four remainders, a 16-byte entry; three products -- leading parts, and either
+// one with the other's remainders -- give 22 bits of each factor.  Probabilities are two bf16 numbers each, values are bf16 as they are.
+//
+// No decoded key is written anywhere and no barrier is in the loop: a wavefront owns steps of 32 tokens (its records and value rows
+// staged in LDS of its own) and 32 query rows, 16 at head dimension 256; the wavefronts of a workgroup take the steps of a segment in
+// turn, and their (m, l, acc) join at its end.  At most 256 workgroups, one a compute unit (the tables fill LDS and are built once),
+// walk the segments: the prefix's first, then the own ones; the row groups that read the same tokens on one die.
+//
+// What bounds it: the vector units, LDS and the matrix cores, in turns, with two wavefronts a SIMD to hide one behind the other (the
+// accumulators and the queries' operands leave room for no third).  At d = 128, 3 bits, a step of 32 tokens and 32 rows is 92 matrix
+// instructions (1470 clocks) and some 260 vector ones (1040), and two wavefronts take 5800 for two; with every page the same (no memory)
+// a call of 75 us takes 70, with table reads that never meet on a bank 73, with both 64.
 #ifndef OCTOPUS_PREFIX_HPP_
 #define OCTOPUS_PREFIX_HPP_
 
@@ -553,13 +562,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             for (int rb = 0; rb < LIVE; ++rb)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) score[e / 4][rb][e % 4] *= gamma[e / 4][e % 4];
-            // nothing reads this step's records any more: the next step's take their place
-            if (more) {
-                __builtin_amdgcn_wave_barrier();
-                store_records();
-                __builtin_amdgcn_wave_barrier();
-                read_words();
-            }
             // tokens past the sequence's end, or that a row does not see for causality
             if ((step + 1) * kPrefixKeys > all_see) {
 #pragma unroll
@@ -592,9 +594,31 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] *= alpha;
                 }
             }
-            // The values have arrived; the records of the step after the next are asked for only now, as waiting for what a load
-            // wrote to LDS waits for every load. Rows past the last token are made zeros: their probabilities are zero, but what
-            // lies there may be no number.
+            prefix_bf16x8_t p_hi[LIVE], p_lo[LIVE];
+#pragma unroll
+            for (int rb = 0; rb < LIVE; ++rb) {
+                uint32_t ph[4], pl[4];
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = exp2_raw(fmaf(score[e / 4][rb][e % 4], factor[rb], -m_ref[rb]));
+                    const float p1 = exp2_raw(fmaf(score[e / 4][rb][e % 4 + 1], factor[rb], -m_ref[rb]));
+                    l_run[rb] += p0 + p1;
+                    // two bf16 numbers, each rounded to the nearest, whose sum is p to 2^-18: the values are bf16
+                    ph[e / 2] = bf16_pair(p0, p1);
+                    pl[e / 2] = bf16_pair(p0 - bf16_lo(ph[e / 2]), p1 - bf16_hi(ph[e / 2]));
+                }
+                p_hi[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[0], ph[1], ph[2], ph[3]));
+                p_lo[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+            }
+            // nothing reads this step's records any more: the next step's take their place
+            if (more) {
+                __builtin_amdgcn_wave_barrier();
+                store_records();
+                __builtin_amdgcn_wave_barrier();
+                read_words();
+            }
+            // The values have arrived. Rows past the last token are made zeros: their probabilities are zero, but what lies there may
+            // be no number.
             if constexpr (!C::VREG) wait_loads<0>();
             const int last = len - 1 - step * kPrefixKeys;
             if (last < kPrefixKeys - 1) {
@@ -651,22 +675,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             unsigned char *vat = vals + (row % C::NVAL) * C::VST + (row / C::NVAL) * (2 * D) + (n % 4) * 8;
             constexpr int SECOND = (16 / C::NVAL) * (2 * D);   // 16 rows on
             static_assert(16 % C::NVAL == 0, "16 rows on is a whole number of pieces on");
-            prefix_bf16x8_t p_hi[LIVE], p_lo[LIVE];
-#pragma unroll
-            for (int rb = 0; rb < LIVE; ++rb) {
-                uint32_t ph[4], pl[4];
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float p0 = exp2_raw(fmaf(score[e / 4][rb][e % 4], factor[rb], -m_ref[rb]));
-                    const float p1 = exp2_raw(fmaf(score[e / 4][rb][e % 4 + 1], factor[rb], -m_ref[rb]));
-                    l_run[rb] += p0 + p1;
-                    // two bf16 numbers, each rounded to the nearest, whose sum is p to 2^-18: the values are bf16
-                    ph[e / 2] = bf16_pair(p0, p1);
-                    pl[e / 2] = bf16_pair(p0 - bf16_lo(ph[e / 2]), p1 - bf16_hi(ph[e / 2]));
-                }
-                p_hi[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[0], ph[1], ph[2], ph[3]));
-                p_lo[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
-            }
             union channels_t { s16x4_t h[2]; prefix_bf16x8_t b; } v[AHEAD_V];
             auto ask_values = [&](int cb) __attribute__((always_inline)) {
                 v[cb % AHEAD_V].h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(vat + 32 * cb));
