@@ -69,13 +69,13 @@ struct PrefixCfg {
     static constexpr bool VREG = D == 256;
     static constexpr int VAL = NVAL * VST;                         // bytes of a step's values
     // Query operands in LDS: a row's leading parts and its remainders; rows 16 bytes apart beyond their size, so that the 16 rows read
-    // at once lie on all banks.  The wavefronts' results: rows 16 bytes apart for the same reason.  Both take the values' place.
+    // at once lie on all banks.  The wavefronts' results, which take the values' place: rows 16 bytes apart for the same reason.
     static constexpr int QST = 2 * 4 * KS * 16 + 16;
     static constexpr int OST = D + 4;                              // floats
-    static constexpr int PLACE = (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL) > NW * 16 * OST * 4 ? (ROWS * QST > NW * VAL ? ROWS * QST : NW * VAL)
-                                                                                               : NW * 16 * OST * 4;
+    static constexpr int STAGED = ROWS * QST > NW * REC ? ROWS * QST : NW * REC;
+    static constexpr int PLACE = NW * VAL > NW * 16 * OST * 4 ? NW * VAL : NW * 16 * OST * 4;
     // Copies of the tables' entries, 16 bytes apart, in what is left of LDS (4 KB of it for what is small).
-    static constexpr int LEFT = 160 * 1024 - PLACE - NW * REC - 4096;
+    static constexpr int LEFT = 160 * 1024 - PLACE - STAGED - 4096;
     static constexpr int R0 = rep(E0 * 16, P::NCLASS == 2 ? 32768 : (LEFT < 65536 ? LEFT : 65536));
     static constexpr int R1 = P::NCLASS == 2 ? rep(E1 * 16, 16384) : 1;
     // The transform of the queries: eight coordinates a thread.
@@ -87,7 +87,7 @@ struct PrefixSmem {
     using C = PrefixCfg<P>;
     uint4 tab0[C::E0 * C::R0];
     uint4 tab1[P::NCLASS == 2 ? C::E1 * C::R1 : 1];
-    unsigned char rec[C::NW][C::REC];
+    unsigned char rec[C::STAGED];  // a segment's query operands, then the wavefronts' staged records
     float ml[C::NW][C::ROWS][2];
     float factor[C::ROWS];         // of a row's scores
     float c_xi[P::NCLASS][1 << (P::BD0 > P::BD1 ? P::BD0 : P::BD1)];
@@ -185,22 +185,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     __shared__ __attribute__((aligned(16))) unsigned char place[C::PLACE];   // (an object of its own: reads of the tables need not wait for it)
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
 
-    // levels, a lane each, then the tables
-    {
-        typedef const float __attribute__((address_space(4))) *arg_t;
-        arg_t arg = (arg_t)__builtin_amdgcn_kernarg_segment_ptr();
-        constexpr int NX = sizeof(sm.c_xi[0]) / 4, NR = sizeof(sm.c_rho[0]) / 4;
-        const int lane = threadIdx.x & 63;
-        if (wave < P::NCLASS) {
-            const float xi = arg[offsetof(DeviceBooks, c_xi) / 4 + wave * kMaxLevels + lane], rho = arg[offsetof(DeviceBooks, c_rho) / 4 + wave * kMaxLevels + lane];
-            if (lane < NX) sm.c_xi[wave][lane] = xi;
-            if (lane < NR) sm.c_rho[wave][lane] = rho * (C::J0 ? 1.0f : kUnitScale);
-        }
-    }
-    lds_barrier();
-    build_prefix_tables<P>(sm, threadIdx.x);
-
-    unsigned char *stage = sm.rec[wave], *vals = place + wave * C::VAL;
+    unsigned char *stage = sm.rec + wave * C::REC, *vals = place + wave * C::VAL;
     constexpr int DQ0 = C::T0 * 2 * P::BD0, NQ0 = C::T0 * P::BN0, DQ1 = C::T1 * 2 * P::BD1, NQ1 = C::T1 * P::BN1;
     using SD0 = QuarterStream<P::DIR0_BIT, DQ0>;
     using SN0 = QuarterStream<P::NRM0_BIT, NQ0>;
@@ -212,6 +197,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     // (its sign is the queries': a row's factor is not negative, so the largest product is the largest score's)
     const float norm = fabsf(shp.scale) * kLog2e * (D == 64 ? 0.125f : (D == 128 ? 0.08838834764831845f : 0.0625f)) / kUnitScale;
 
+    bool built = false;                  // the tables
     for (int seg = blockIdx.x; seg < shp.n_segments; seg += gridDim.x) {
         // (opaque: what follows from a lane's number is computed for each segment, not kept -- in scratch memory, whose reads would
         // wait for the values on their way -- from the kernel's start)
@@ -241,6 +227,26 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         const int rows = shared ? all_rows : own_rows, row0 = grp * C::ROWS;
         const int live = min(RB, (rows - row0 + 15) / 16);              // blocks of 16 rows with rows
 
+        // ---- the levels and the segment's queries, asked for with the pages ----
+        float xi = 0.0f, rho = 0.0f;
+        if (!built && wave < P::NCLASS) {
+            typedef const float __attribute__((address_space(4))) *arg_t;
+            arg_t arg = (arg_t)__builtin_amdgcn_kernarg_segment_ptr();
+            xi = arg[offsetof(DeviceBooks, c_xi) / 4 + wave * kMaxLevels + lane];
+            rho = arg[offsetof(DeviceBooks, c_rho) / 4 + wave * kMaxLevels + lane];
+        }
+        const int qc = tid % C::QLANES;                  // coordinates 8 qc .. + 7
+        prefix_u32x4_t asked[C::QPASS][2];
+        uint32_t sbits = shp.signs[kvh * (D / 8) + qc];
+#pragma unroll
+        for (int p = 0; p < C::QPASS; ++p) {
+            typedef uint32_t u32x4a_t __attribute__((ext_vector_type(4), aligned(4)));
+            const int row = min(row0 + tid / C::QLANES + p * C::QROWS, rows - 1);
+            const int64_t at = ((static_cast<int64_t>(seq) * shp.n_q + row / hpk) * shp.n_q_heads + kvh * hpk + row % hpk) * D + 8 * qc;
+            const unsigned char *src = static_cast<const unsigned char *>(shp.q) + at * (shp.q_is_bf16 ? 2 : 4);
+            asked[p][0] = *reinterpret_cast<const u32x4a_t *>(src);
+            asked[p][1] = *reinterpret_cast<const u32x4a_t *>(src + (shp.q_is_bf16 ? 0 : 16));
+        }
         // ---- a step's records, from memory to registers and from there to LDS; its values, from memory to LDS ----
         prefix_u32x4_t rec[C::NREC];
         // the pages of the wavefront's next 64 steps, one a lane
@@ -285,8 +291,17 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             for (int e = 0; e < C::NVAL; ++e) *reinterpret_cast<prefix_u32x4_t *>(vals + e * C::VST + lane * 16) = val[e];
         };
         const bool work = begin + wave < end;
+        if (work) hold_pages(begin + wave);
+        if (!built && wave < P::NCLASS) {    // (they have arrived with the pages; a lane each)
+            constexpr int NX = sizeof(sm.c_xi[0]) / 4, NR = sizeof(sm.c_rho[0]) / 4;
+            if (lane < NX) sm.c_xi[wave][lane] = xi;
+            if (lane < NR) sm.c_rho[wave][lane] = rho * (C::J0 ? 1.0f : kUnitScale);
+        }
+        // (all of it is waited for here, where the pages are, and not behind the records and values)
+        asm volatile("" : "+v"(xi), "+v"(rho), "+v"(held), "+v"(sbits));
+#pragma unroll
+        for (int p = 0; p < C::QPASS; ++p) asm volatile("" : "+v"(asked[p][0]), "+v"(asked[p][1]));
         if (work) {
-            hold_pages(begin + wave);
             load_records(begin + wave, page_of(begin + wave));
             if constexpr (C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
@@ -308,20 +323,12 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
         };
 
-        // ---- the segment's queries: asked for before the tables are complete, rotated, then as operands through LDS ----
-        const int qc = tid % C::QLANES;                  // coordinates 8 qc .. + 7
-        prefix_u32x4_t asked[C::QPASS][2];
-        const uint32_t sbits = shp.signs[kvh * (D / 8) + qc];
-#pragma unroll
-        for (int p = 0; p < C::QPASS; ++p) {
-            typedef uint32_t u32x4a_t __attribute__((ext_vector_type(4), aligned(4)));
-            const int row = min(row0 + tid / C::QLANES + p * C::QROWS, rows - 1);
-            const int64_t at = ((static_cast<int64_t>(seq) * shp.n_q + row / hpk) * shp.n_q_heads + kvh * hpk + row % hpk) * D + 8 * qc;
-            const unsigned char *src = static_cast<const unsigned char *>(shp.q) + at * (shp.q_is_bf16 ? 2 : 4);
-            asked[p][0] = *reinterpret_cast<const u32x4a_t *>(src);
-            asked[p][1] = *reinterpret_cast<const u32x4a_t *>(src + (shp.q_is_bf16 ? 0 : 16));
+        // ---- the tables, while the records and values are on their way; the queries rotated, and as operands through LDS ----
+        if (!built) {
+            lds_barrier();
+            build_prefix_tables<P>(sm, tid);
+            built = true;
         }
-        lds_barrier();                 // tables complete; the last segment's results have been read
 #pragma unroll
         for (int p = 0; p < C::QPASS; ++p) {
             const int local = tid / C::QLANES + p * C::QROWS;
@@ -366,7 +373,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     const bool second = P::NCLASS == 2 && t >= P::NT0;
                     const int of = second ? t - P::NT0 : t, each = second ? (C::T1 > 0 ? C::T1 : 1) : C::T0;
                     const int at = of % each + (second ? C::T0 : 0);
-                    unsigned char *to = place + local * C::QST + (of / each) * (KS * 16) + (3 * at + c % 3) * 2;
+                    unsigned char *to = sm.rec + local * C::QST + (of / each) * (KS * 16) + (3 * at + c % 3) * 2;
                     const float y = ldexpf(x[e], -ex);
                     const _Float16 hi = static_cast<_Float16>(y), lo = static_cast<_Float16>(y - static_cast<float>(hi));
                     *reinterpret_cast<_Float16 *>(to) = hi;
@@ -374,6 +381,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 }
             }
         }
+        // (not before: writes to LDS wait for what comes to LDS from memory)
+        if (!C::VREG && work) load_values(begin + wave, page_of(begin + wave));
         lds_barrier();
         auto walk = [&](auto live_) __attribute__((always_inline)) {
         constexpr int LIVE = decltype(live_)::value;   // blocks of 16 rows with rows
@@ -385,7 +394,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         for (int rb = 0; rb < LIVE; ++rb) {
             // (places that no coordinate has: those of triplets past a class's last, of coordinates past the last and behind a lane
             // group's triplets; what lies there is left over)
-            const unsigned char *from = place + (rb * 16 + n) * C::QST + g * (KS * 16);
+            const unsigned char *from = sm.rec + (rb * 16 + n) * C::QST + g * (KS * 16);
             static_for<0, KS>([&](auto kk_) {
                 constexpr int kk = decltype(kk_)::value;
                 uint4 h = *reinterpret_cast<const uint4 *>(from + kk * 16), l = *reinterpret_cast<const uint4 *>(from + 4 * KS * 16 + kk * 16);
@@ -425,7 +434,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             }
         }
         all_see = __builtin_amdgcn_readfirstlane(all_see);
-        lds_barrier();                 // the operands have been read: the values' places are the wavefronts' own now
+        lds_barrier();                 // the operands have been read: the staging areas are the wavefronts' own now
 
         // ---- the steps ----
         float m_ref[LIVE], l_run[LIVE];
@@ -460,7 +469,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 load_records(begin + wave + NW, page_of(begin + wave + NW));
                 if constexpr (C::VREG) load_values(begin + wave + NW, page_of(begin + wave + NW));
             }
-            if constexpr (!C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
         for (int step = begin + wave; step < end; step += NW) {
             const bool more = step + NW < end, two_more = step + 2 * NW < end;
