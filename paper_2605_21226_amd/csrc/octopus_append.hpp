@@ -7,7 +7,8 @@
 // key that the encoder takes: what octopus_encode_paged computes of rotated keys, without their rounding to bf16 in between.
 //
 // What bounds it: memory, for long prompts -- queries, keys and values come and go once, the records are a quarter of the keys -- and
-// latency for a few tokens.
+// latency for a few tokens.  Measured at d = 128, 3 bits, 32 query and 8 KV heads, bf16: 15877 tokens, 366 MB, in 97 us, 3.8 TB/s
+// where a copy reaches 5.0; a token of each of 64 sequences, 0.7 MB, in 6.6 us, all latency.
 #ifndef OCTOPUS_APPEND_HPP_
 #define OCTOPUS_APPEND_HPP_
 

@@ -3,7 +3,8 @@
 //
 // A workgroup takes a 64-token tile of one (sequence, KV head), the encoder's phases the other way round: records unpacked a key per
 // lane, a share of the triplets per wavefront; the transform's far stages a key per lane; its near ones eight coordinates a thread,
-// which then have the order of the output row.  Bound by memory (a row out is 256 bytes at d = 128 in bf16, its record 64).
+// which then have the order of the output row.  Bound by memory (a row out is 256 bytes at d = 128 in bf16, its record 64): 15877
+// tokens of 8 KV heads, 106 MB, take 21.8 us, 4.8 TB/s; at d = 256 with quantised values to fp32, 41 MB of ragged tails, 15.9.
 #ifndef OCTOPUS_READ_HPP_
 #define OCTOPUS_READ_HPP_
 
@@ -20,7 +21,8 @@ struct ReadSmem {
     float c_rho[P::NCLASS][kMaxLevels];
 };
 
-// (wavefronts a workgroup: at head dimension 256, whose tile in LDS lets two workgroups into a compute unit, twice as many)
+// (wavefronts a workgroup: at head dimension 256, whose tile in LDS lets two workgroups into a compute unit, twice as many -- 23.1 us
+// with four for the ragged tails, 16.3 with eight; at 128 eight make no difference)
 constexpr int read_waves(int d) { return d == 256 ? 8 : 4; }
 
 template <class P>

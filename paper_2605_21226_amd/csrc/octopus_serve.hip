@@ -40,7 +40,7 @@ int launch_read(const octopus_codebooks_t &cb, const ReadCall &a, void *stream) 
 // out = sum_i 2^(m_i - M) acc_i / sum_i 2^(m_i - M) l_i over an output row's partial results, the prefix's and the own ones; zeros where
 // no token was seen.  Rows past a sequence's q_lens are left as they were.  A workgroup per row, whose time is the latency of three
 // dependent reads: D / 4 threads read a partial result, 16 bytes each, and the 512 / D groups of them take every so manieth, 16 on their way at once; the groups'
-// sums meet in LDS.
+// sums meet in LDS.  512 rows of 17 partial results at d = 128 (4.5 MB) take 5.3 us; a wavefront per row took 9.0.
 constexpr int kMergeThreads = 128;
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void prefix_merge_kernel(PrefixShape s, const int32_t *__restrict__ prefix_len,
