@@ -515,14 +515,15 @@ int octopus_attn_decode_paged_qjl(const octopus_codebooks_t *cb,
  *                encoded as it leaves them (octopus_encode_paged of keys rotated in bf16 sees them rounded).
  *   q            device, [n_seq][n_new][n_q_heads] rows like k (q_dtype, strides, alignment), or NULL: none.  q_out: device,
  *                [n_seq][n_new][n_q_heads][d] contiguous, q_out_dtype F32/BF16, 16-byte aligned: the rotated queries (rope NULL: q
- *                itself), as octopus_attn_decode_paged and octopus_attn_decode_paged_prefix take them.
+ *                itself), as octopus_attn_decode_paged and octopus_attn_decode_paged_prefix take them.  It may be q, where that is contiguous and of the
+ *                same type.
  *   signs, k_pool, n_pages, block_table, max_pages_per_seq, start_pos   as for octopus_encode_paged: token t of sequence s goes to slot
  *                start_pos[s] + t; slots past max_pages_per_seq * 64 are not written.
  *   v_pool       v_bits 0: bf16 pages [n_pages][n_kv_heads][64][d] (fp32 values are rounded to the nearest); v_bits 2..4: rows quantised
  *                as by octopus_encode_values_paged(bits v_bits, group v_group), byte for byte.
  * One launch; two with quantised values.  Codebooks: those octopus_build_codebooks returns (EUNSUPPORTED for edited ones).
- * Errors: EINVAL (also n_seq or n_kv_heads above 65535, and more than 2^21 (tile, KV head, sequence) triples or runs of 16 tokens by
- * eight rows), EUNSUPPORTED, EHIP. */
+ * Errors: EINVAL (also n_seq or n_kv_heads above 65535, more than 4096 value groups a token, and more than 2^21 (tile, KV head,
+ * sequence) triples or runs of 16 tokens by eight rows), EUNSUPPORTED, EHIP. */
 typedef struct octopus_rope {
     const float *table;
     int64_t n_pos;

@@ -11,6 +11,11 @@ namespace {
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
+// of the partial results' (reference, sum) pairs and rows
+size_t prefix_bytes(int64_t partials, int32_t d) {
+    return 256 + up256(partials * 2 * sizeof(float)) + up256(partials * static_cast<size_t>(d) * sizeof(float));
+}
+
 bool pages_ok(const void *table, int32_t pages) {
     return table != nullptr && aligned(table, 4) && pages >= 1 && pages <= INT32_MAX / OCTOPUS_TILE;
 }
@@ -83,7 +88,7 @@ size_t octopus_attn_prefix_workspace(const octopus_codebooks_t *cb, int32_t n_se
     if (prefix_args(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len) != OCTOPUS_OK) return 0;
     int64_t partials = 0;
     make_prefix_shape(cb->plan, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len, &partials);
-    return 256 + up256(partials * 2 * sizeof(float)) + up256(partials * static_cast<size_t>(cb->plan.head_dim) * sizeof(float));
+    return prefix_bytes(partials, cb->plan.head_dim);
 }
 
 int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb, const void *q, int32_t q_dtype, int32_t n_seq, int32_t n_q_heads,
@@ -110,10 +115,9 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb, const void *
     if (!aligned(q, 4) || !aligned(out, 4) || !aligned(k_pool, 16) || !aligned(v_pool, 16) ||
         !aligned(q_lens, 4) || !std::isfinite(scale))
         return OCTOPUS_EINVAL;
-    const size_t need = octopus_attn_prefix_workspace(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len);
-    if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need) return OCTOPUS_EWORKSPACE;
     int64_t partials = 0;
     PrefixShape s = make_prefix_shape(cb->plan, n_seq, n_q_heads, n_kv_heads, n_q, max_prefix, max_len, &partials);
+    if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < prefix_bytes(partials, cb->plan.head_dim)) return OCTOPUS_EWORKSPACE;
     s.max_pages = max_pages_per_seq;
     s.n_pages = n_pages;
     s.causal = causal;

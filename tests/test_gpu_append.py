@@ -313,3 +313,28 @@ def test_appending_on_another_stream():
         t.qkv.copy_(kept)
         t.append(stream=stream)
     assert torch.equal(s.k_pool, t.k_pool) and torch.equal(s.v_pool, t.v_pool) and torch.equal(s.q_out, t.q_out)
+
+
+@pytest.mark.parametrize("v_bits,v_group", [(0, 0), (3, 16)])
+def test_reading_keys_or_values_alone(v_bits, v_group):
+    s = Setup(128, 3, 2, 2, 1, 70, [5, 64], v_bits=v_bits, v_group=v_group)
+    s.append()
+    v_pool = s.v_pool if v_bits else s.v_pool.view(torch.bfloat16)
+    both, alone = [torch.zeros((2, 70, 2, 128), device=DEV) for _ in range(2)], [torch.zeros((2, 70, 2, 128), device=DEV) for _ in range(2)]
+    args = dict(start_pos=s.start_dev, v_bits=v_bits, v_group=v_group)
+    binding.octopus_read_paged(s.cb, s.signs_dev, s.k_pool, v_pool, s.n_pages, s.block_dev, *both, **args)
+    binding.octopus_read_paged(s.cb, s.signs_dev, s.k_pool, None, s.n_pages, s.block_dev, alone[0], None, **args)
+    binding.octopus_read_paged(s.cb, None, None, v_pool, s.n_pages, s.block_dev, None, alone[1], **args)
+    torch.cuda.synchronize()
+    assert torch.equal(both[0], alone[0]) and torch.equal(both[1], alone[1]) and float(both[0].abs().min(dim=-1).values.max()) > 0
+
+
+def test_queries_rotated_in_place_and_without_rotation():
+    s = Setup(128, 3, 2, 2, 4, 50, [5, 64], new_lens=[50, 20])
+    s.append()
+    own = s.q_dev.contiguous()
+    s.append(q=own, q_out=own)                                 # the rows are the call's own to overwrite
+    assert torch.equal(own[0], s.q_out[0]) and torch.equal(own[1, :20], s.q_out[1, :20]) and torch.equal(own[1, 20:], s.q_dev[1, 20:])
+    plain = torch.full_like(s.q_out, 7.0)
+    s.append(rope=None, rope_pos=None, q_out=plain)
+    assert torch.equal(plain[0], s.q_dev[0]) and bool((plain[1, 20:] == 7.0).all())

@@ -289,3 +289,17 @@ def test_profile_events_enclose_the_attention():
     assert 0.0 < before.elapsed_time(after) < 1000.0
     first = before.elapsed_time(after)
     assert torch.equal(b.call(), want) and before.elapsed_time(after) == first       # one call only
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_shapes(seed):
+    rng = np.random.default_rng(1000 + seed)
+    d, bits = int(rng.choice([64, 128, 256])), float(rng.choice([1, 1.5, 2, 2.5, 3, 4]))
+    n_kv, g, n_q = int(rng.integers(1, 4)), int(rng.choice([1, 2, 3, 4, 5, 8])), int(rng.choice([1, 1, 2, 3, 7, 11]))
+    n_seq, prefix = int(rng.integers(1, 6)), int(rng.choice([0, 1, 31, 64, 97, 200, 450]))
+    lens = [int(x) for x in rng.integers(0, 150, n_seq) * rng.integers(0, 2, n_seq) + rng.integers(0, 12, n_seq)]
+    q_lens = [int(x) for x in rng.integers(0, n_q + 1, n_seq)] if seed % 2 else None
+    b = Batch(d, bits, g * n_kv, n_kv, n_q, prefix, lens, seed=seed, q_dtype="fp32" if seed % 3 == 0 else "bf16")
+    causal = bool(rng.integers(0, 2))
+    b.check(b.call(q_lens=q_lens, causal=causal), q_lens=q_lens, causal=causal)
+    b.check(b.call(q_lens=q_lens, causal=causal, max_prefix=64 * b.pp, max_len=64 * b.op), q_lens=q_lens, causal=causal)
