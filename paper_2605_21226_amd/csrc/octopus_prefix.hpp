@@ -84,10 +84,15 @@ struct PrefixCfg {
 };
 
 template <class P>
-struct PrefixSmem {
+struct PrefixTables {
     using C = PrefixCfg<P>;
     uint4 tab0[C::E0 * C::R0];
     uint4 tab1[P::NCLASS == 2 ? C::E1 * C::R1 : 1];
+};
+
+template <class P>
+struct PrefixSmem {
+    using C = PrefixCfg<P>;
     unsigned char rec[C::STAGED];  // a segment's query operands, then the wavefronts' staged records
     float ml[C::NW][C::ROWS][2];
     float factor[C::ROWS];         // of a row's scores
@@ -134,7 +139,7 @@ __device__ __forceinline__ void wait_lds() {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <class P>
-__device__ __forceinline__ void build_prefix_tables(PrefixSmem<P> &sm, int tid) {
+__device__ __forceinline__ void build_prefix_tables(PrefixSmem<P> &sm, PrefixTables<P> &tb, int tid) {
     using C = PrefixCfg<P>;
     auto one = [&](auto bd_, auto bn_, auto joint_, uint4 *tab, const float *c_xi, const float *c_rho, auto entries_, auto rep_) {
         constexpr int BD = decltype(bd_)::value, BN = decltype(bn_)::value, E = decltype(entries_)::value, REP = decltype(rep_)::value;
@@ -155,10 +160,10 @@ __device__ __forceinline__ void build_prefix_tables(PrefixSmem<P> &sm, int tid) 
         }
     };
     using std::integral_constant;
-    one(integral_constant<int, P::BD0>{}, integral_constant<int, P::BN0>{}, integral_constant<bool, C::J0>{}, sm.tab0, sm.c_xi[0], sm.c_rho[0],
+    one(integral_constant<int, P::BD0>{}, integral_constant<int, P::BN0>{}, integral_constant<bool, C::J0>{}, tb.tab0, sm.c_xi[0], sm.c_rho[0],
         integral_constant<int, C::E0>{}, integral_constant<int, C::R0>{});
     if constexpr (P::NCLASS == 2)
-        one(integral_constant<int, P::BD1>{}, integral_constant<int, P::BN1>{}, integral_constant<bool, C::J1>{}, sm.tab1, sm.c_xi[1],
+        one(integral_constant<int, P::BD1>{}, integral_constant<int, P::BN1>{}, integral_constant<bool, C::J1>{}, tb.tab1, sm.c_xi[1],
             sm.c_rho[1], integral_constant<int, C::E1>{}, integral_constant<int, C::R1>{});
 }
 
@@ -183,6 +188,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     constexpr int CB = D / 16;                       // blocks of 16 channels
     constexpr int64_t TILEB = P::GRANULES * kWave * 16, VTILEB = static_cast<int64_t>(kWave) * D * 2;
     __shared__ __attribute__((aligned(16))) PrefixSmem<P> sm;
+    __shared__ __attribute__((aligned(16))) PrefixTables<P> tb;
     __shared__ __attribute__((aligned(16))) unsigned char place[C::PLACE];   // (an object of its own: reads of the tables need not wait for it)
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
 
@@ -327,7 +333,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         // ---- the tables, while the records and values are on their way; the queries rotated, and as operands through LDS ----
         if (!built) {
             lds_barrier();
-            build_prefix_tables<P>(sm, tid);
+            build_prefix_tables<P>(sm, tb, tid);
             built = true;
         }
 #pragma unroll
@@ -485,21 +491,21 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                         // the code is a whole byte and the entry's offset has it as its second byte, above norm code and copy
                         const uint32_t low = nrm << (4 + C::log2i(C::R0)) | static_cast<uint32_t>(lane & (C::R0 - 1)) << 4;
                         const uint32_t at_byte = __builtin_amdgcn_perm(wd0[kb][at / 4], low, 0x0c0c0400u + ((at % 4) << 8));
-                        return *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(sm.tab0) + at_byte);
+                        return *reinterpret_cast<const uint4 *>(reinterpret_cast<const unsigned char *>(tb.tab0) + at_byte);
                     } else if constexpr (C::J0) {
                         constexpr int NS = C::log2i(C::R0);
                         const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0[kb]);
-                        return sm.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
+                        return tb.tab0[(dir << (NS + P::BN0)) + (nrm << NS) + (lane & (C::R0 - 1))];
                     } else {
                         const uint32_t dir = field_clamped<at * 2 * P::BD0, 2 * P::BD0>(wd0[kb]);
-                        uint4 d4 = sm.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
+                        uint4 d4 = tb.tab0[dir * C::R0 + (lane & (C::R0 - 1))];
                         d4.w = __float_as_uint(sm.c_rho[0][nrm]);
                         return d4;
                     }
                 } else if constexpr (P::NCLASS == 2) {
                     constexpr int a1 = at - C::T0, NS = C::log2i(C::R1);
                     const uint32_t dir = field_clamped<a1 * 2 * P::BD1, 2 * P::BD1>(wd1[kb]), nrm = field_clamped<a1 * P::BN1, P::BN1>(wn1[kb]);
-                    return sm.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
+                    return tb.tab1[(dir << (NS + P::BN1)) + (nrm << NS) + (lane & (C::R1 - 1))];
                 }
             };
             // (tables without norms: the triplet is put together here)
