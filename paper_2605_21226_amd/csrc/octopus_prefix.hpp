@@ -93,7 +93,6 @@ struct PrefixTables {
 template <class P>
 struct PrefixSmem {
     using C = PrefixCfg<P>;
-    unsigned char rec[C::STAGED];  // a segment's query operands, then the wavefronts' staged records
     float ml[C::NW][C::ROWS][2];
     float factor[C::ROWS];         // of a row's scores
     float c_xi[P::NCLASS][1 << (P::BD0 > P::BD1 ? P::BD0 : P::BD1)];
@@ -189,10 +188,11 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     constexpr int64_t TILEB = P::GRANULES * kWave * 16, VTILEB = static_cast<int64_t>(kWave) * D * 2;
     __shared__ __attribute__((aligned(16))) PrefixSmem<P> sm;
     __shared__ __attribute__((aligned(16))) PrefixTables<P> tb;
+    __shared__ __attribute__((aligned(16))) unsigned char staged[C::STAGED];   // a segment's query operands, then the wavefronts' staged records
     __shared__ __attribute__((aligned(16))) unsigned char place[C::PLACE];   // (an object of its own: reads of the tables need not wait for it)
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
 
-    unsigned char *stage = sm.rec + wave * C::REC, *vals = place + wave * C::VAL;
+    unsigned char *stage = staged + wave * C::REC, *vals = place + wave * C::VAL;
     constexpr int DQ0 = C::T0 * 2 * P::BD0, NQ0 = C::T0 * P::BN0, DQ1 = C::T1 * 2 * P::BD1, NQ1 = C::T1 * P::BN1;
     using SD0 = QuarterStream<P::DIR0_BIT, DQ0>;
     using SN0 = QuarterStream<P::NRM0_BIT, NQ0>;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             asked[p][1] = *reinterpret_cast<const u32x4a_t *>(src + (shp.q_is_bf16 ? 0 : 16));
         }
         // ---- a step's records, from memory to registers and from there to LDS; its values, from memory to LDS ----
-        prefix_u32x4_t rec[C::NREC];
+        prefix_u32x4_t rec[C::NREC], second[C::NREC];
         // the pages of the wavefront's next 64 steps, one a lane
         int held = 0, held_from = 0;
         auto hold_pages = [&](int step) __attribute__((always_inline)) {
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         };
         constexpr bool HALF = P::GRANULES % 2 != 0;       // (an odd number of granules: the last piece is half the lanes')
         const uint32_t rec_at = (lane / kPrefixKeys) * (kWave * 16) + (lane % kPrefixKeys) * 16;
-        auto load_records = [&](int step, int page) __attribute__((always_inline)) {
+        auto load_records = [&](prefix_u32x4_t (&rec)[C::NREC], int step, int page) __attribute__((always_inline)) {
             const unsigned char *src = k_pool + (static_cast<int64_t>(page) * shp.n_kv_heads + kvh) * TILEB + (step & 1) * (kPrefixKeys * 16);
 #pragma unroll
             for (int e = 0; e < C::NREC; ++e)
@@ -309,7 +309,9 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
 #pragma unroll
         for (int p = 0; p < C::QPASS; ++p) asm volatile("" : "+v"(asked[p][0]), "+v"(asked[p][1]));
         if (work) {
-            load_records(begin + wave, page_of(begin + wave));
+            load_records(rec, begin + wave, page_of(begin + wave));
+            // (of the second step, too: before the first values, which the loop's waits for records are not to wait for)
+            if (begin + wave + NW < end) load_records(second, begin + wave + NW, page_of(begin + wave + NW));
             if constexpr (C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
 
@@ -380,7 +382,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     const bool second = P::NCLASS == 2 && t >= P::NT0;
                     const int of = second ? t - P::NT0 : t, each = second ? (C::T1 > 0 ? C::T1 : 1) : C::T0;
                     const int at = of % each + (second ? C::T0 : 0);
-                    unsigned char *to = sm.rec + local * C::QST + (of / each) * (KS * 16) + (3 * at + c % 3) * 2;
+                    unsigned char *to = staged + local * C::QST + (of / each) * (KS * 16) + (3 * at + c % 3) * 2;
                     const float y = ldexpf(x[e], -ex);
                     const _Float16 hi = static_cast<_Float16>(y), lo = static_cast<_Float16>(y - static_cast<float>(hi));
                     *reinterpret_cast<_Float16 *>(to) = hi;
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         for (int rb = 0; rb < LIVE; ++rb) {
             // (places that no coordinate has: those of triplets past a class's last, of coordinates past the last and behind a lane
             // group's triplets; what lies there is left over)
-            const unsigned char *from = sm.rec + (rb * 16 + n) * C::QST + g * (KS * 16);
+            const unsigned char *from = staged + (rb * 16 + n) * C::QST + g * (KS * 16);
             static_for<0, KS>([&](auto kk_) {
                 constexpr int kk = decltype(kk_)::value;
                 uint4 h = *reinterpret_cast<const uint4 *>(from + kk * 16), l = *reinterpret_cast<const uint4 *>(from + 4 * KS * 16 + kk * 16);
@@ -472,9 +474,10 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             __builtin_amdgcn_wave_barrier();
             if constexpr (C::VREG) store_values();
             read_words();
-            if (begin + wave + NW < end) {
-                load_records(begin + wave + NW, page_of(begin + wave + NW));
-                if constexpr (C::VREG) load_values(begin + wave + NW, page_of(begin + wave + NW));
+#pragma unroll
+            for (int e = 0; e < C::NREC; ++e) rec[e] = second[e];
+            if constexpr (C::VREG) {
+                if (begin + wave + NW < end) load_values(begin + wave + NW, page_of(begin + wave + NW));
             }
         }
         for (int step = begin + wave; step < end; step += NW) {
@@ -716,7 +719,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 // (the records first: they are waited for first, and a wait for them is not one for the values)
                 if (two_more) {
                     if (step + 2 * NW - held_from >= 64 * NW) hold_pages(step + NW);
-                    load_records(step + 2 * NW, page_of(step + 2 * NW));
+                    load_records(rec, step + 2 * NW, page_of(step + 2 * NW));
                     if constexpr (C::VREG) load_values(step + 2 * NW, page_of(step + 2 * NW));
                 }
                 if constexpr (!C::VREG) load_values(step + NW, page_of(step + NW));
