@@ -172,6 +172,7 @@ struct QuarterStream {
     static constexpr int WORDS = (QUARTER_BITS + 31) / 32;
     static constexpr bool ALIGNED = START % 32 == 0 && QUARTER_BITS % 32 == 0;
     static constexpr int READ = ALIGNED ? WORDS : WORDS + 1;
+    static constexpr int END = ((START + 3 * QUARTER_BITS) / 32 + READ) * 4;   // bytes of a record that the last group's quarter reaches
 };
 
 // CAUSAL: rows of a sequence may see fewer of its tokens than others.  (A kernel of its own: what it takes to keep values that are no
@@ -198,6 +199,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     using SN0 = QuarterStream<P::NRM0_BIT, NQ0>;
     using SD1 = QuarterStream<P::DIR1_BIT, (DQ1 > 0 ? DQ1 : 32)>;
     using SN1 = QuarterStream<P::NRM1_BIT, (NQ1 > 0 ? NQ1 : 32)>;
+    static_assert(SD0::END <= C::RST && SN0::END <= C::RST && SD1::END <= C::RST && SN1::END <= C::RST, "within a staged record and its padding");
     const int hpk = shp.n_q_heads / shp.n_kv_heads;
     const int all_rows = shp.n_seq * shp.n_q * hpk, own_rows = shp.n_q * hpk;
     // what a factor of 256 in the keys and the units of log2 make of the caller's scale
@@ -315,7 +317,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             if constexpr (C::VREG) load_values(begin + wave, page_of(begin + wave));
         }
 
-        // (the last quarter's padding may lie past the record, in the 16 bytes between two records or in the next: its terms meet zeros)
+        // (the last quarter may reach past the record, into its padding: those terms meet zeros)
         auto quarter = [&](auto stream_, int start, int quarter_bits, auto &words, int block) __attribute__((always_inline)) {
             using S = decltype(stream_);
             const int bit = start + g * quarter_bits;
