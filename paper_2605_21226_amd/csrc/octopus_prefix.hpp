@@ -18,9 +18,9 @@
 //
 // What bounds it: the vector units, the matrix cores and LDS, in turns, with two wavefronts a SIMD to hide one behind the other (the
 // accumulators and the queries' operands leave room for no third).  16 sequences of 32 heads behind 65531 tokens with 512 own ones, d = 128,
-// 3 bits: 189 MB in 70 us (2.7 TB/s; the copy's rate would be 38), vector units active 48 % of it, matrix cores 35 %, LDS 41 %.  A step of
-// 32 tokens and 32 rows is 92 matrix instructions (1470 clocks) and some 260 vector ones (1040).  Before that, with six operands a key,
-// a call of 77 us took 70 without memory (one page for all), 76 with table reads that never meet on a bank, 64 with both.
+// 3 bits: 189 MB in 69 us (2.7 TB/s; at a copy's rate it would be 38), vector units active 51 % of it, matrix cores 36 %, LDS 41 %.  A step of
+// 32 tokens and 32 rows is 92 matrix instructions (1470 clocks) and some 260 vector ones (1040).  A
+// form of 77 us took 70 without memory (one page for all), 76 with table reads that never meet on a bank, 64 with both.
 #ifndef OCTOPUS_PREFIX_HPP_
 #define OCTOPUS_PREFIX_HPP_
 
