@@ -156,13 +156,15 @@ int launch_decode_vq(const octopus_codebooks_t &cb, const DecodeShape &s, const 
 // sequence's tokens for prefix_rows query rows of one KV head; the prefix's segments come first.
 constexpr int prefix_rows(int head_dim) { return head_dim <= 128 ? 32 : 16; }   // of a workgroup: what its registers hold
 constexpr int prefix_waves(int head_dim) { return head_dim <= 128 ? 8 : 4; }    // of a workgroup: what registers and LDS hold
+constexpr float kNoTokenSeen = -3.402823466e38f;   // reference of a row that has seen none: no finite score lies below it
 struct PrefixShape {
     int32_t n_seq, n_q_heads, n_kv_heads, n_q;
     int32_t max_prefix, max_len, max_pages, n_pages;
     int32_t causal, q_is_bf16;
     const void *q;
     const uint8_t *signs;
-    float scale;
+    float scale_part;       // scale log2(e) / (256 sqrt(d)) is scale_part 2^scale_exp: the part goes into the queries, so that a row's
+    int32_t scale_exp;      // factor is a power of two and takes no score's last bits
     int32_t prefix_groups, prefix_splits, own_groups, own_splits;   // groups of query rows, ranges of tokens
     int32_t prefix_segments, n_segments;
     int64_t own_partials;   // partial results before the first of a sequence's own (one per query row and range)

@@ -35,7 +35,8 @@ typedef uint32_t prefix_u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kPrefixKeys = 32;      // tokens of a step
-constexpr float kUnitScale = 256.0f; // the table's numbers are 256 rho n: the remainders of small ones stay above fp16's denormals
+constexpr float kUnitScale = 256.0f; // the table's numbers are 256 rho n: the remainders of small ones stay above fp16's denormals (the host
+                                     // takes the factor out of the scale again)
 
 template <class P>
 struct PrefixCfg {
@@ -202,9 +203,6 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
     static_assert(SD0::END <= C::RST && SN0::END <= C::RST && SD1::END <= C::RST && SN1::END <= C::RST, "within a staged record and its padding");
     const int hpk = shp.n_q_heads / shp.n_kv_heads;
     const int all_rows = shp.n_seq * shp.n_q * hpk, own_rows = shp.n_q * hpk;
-    // what a factor of 256 in the keys and the units of log2 make of the caller's scale
-    // (its sign is the queries': a row's factor is not negative, so the largest product is the largest score's)
-    const float norm = fabsf(shp.scale) * kLog2e * (D == 64 ? 0.125f : (D == 128 ? 0.08838834764831845f : 0.0625f)) / kUnitScale;
 
     bool built = false;                  // the tables
     for (int seg = blockIdx.x; seg < shp.n_segments; seg += gridDim.x) {
@@ -344,13 +342,12 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         for (int p = 0; p < C::QPASS; ++p) {
             const int local = tid / C::QLANES + p * C::QROWS;
             const bool there = row0 + local < rows;
-            const uint32_t flip = sbits ^ (shp.scale < 0.0f ? 0xffu : 0u);
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const uint32_t two = asked[p][0][e / 2], own = asked[p][e / 4][e % 4];
                 const uint32_t bits = shp.q_is_bf16 ? ((e & 1) ? two & 0xffff0000u : two << 16) : own;
-                x[e] = there ? __uint_as_float(bits ^ ((flip << (31 - e)) & 0x80000000u)) : 0.0f;
+                x[e] = there ? __uint_as_float(bits ^ ((sbits << (31 - e)) & 0x80000000u)) : 0.0f;
             }
 #pragma unroll
             for (int m = 1; m < 8; m <<= 1)
@@ -369,15 +366,21 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     x[e] = (lane & m) ? other - x[e] : x[e] + other;
                 }
             });
-            // a power of two brings the row's largest number into [1/2, 1): fp16 has no range to spare
+            // The scale's sign and mantissa go into the queries.  What is left of it is a row's factor, a power of two: factor score is exact,
+            // so the largest score's probability is 1 whatever its size (a product rounded before the reference is taken from it would
+            // leave up to half a step of the score, which is no number's exponent any more from 2^31 on).  Another power of two brings
+            // the row's largest number into [1/2, 1): fp16 has no range to spare.
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= shp.scale_part;
             float top = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
             static_for<0, C::log2i(C::QLANES)>([&](auto bb) { top = fmaxf(top, lane_xor<(1 << decltype(bb)::value)>(top, lane)); });
             const int ex = top > 0.0f && top < INFINITY ? __builtin_amdgcn_frexp_expf(top) : 0;
             if (C::ROWS % C::QROWS == 0 || local < C::ROWS) {
-                // (not zero, which a scale of zero would make it: what a row does not see has a score of minus infinity, and stays there)
-                if (qc == 0) sm.factor[local] = fmaxf(ldexpf(norm, ex), 1.17549435e-38f);
+                // (neither zero nor infinity: what a row does not see has a score of minus infinity, and stays there, and a score of
+                // zero stays one)
+                if (qc == 0) sm.factor[local] = ldexpf(1.0f, min(max(ex + shp.scale_exp, -126), 127));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int c = 8 * qc + e, t = c / 3;
@@ -452,7 +455,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         f32x4_t oacc[LIVE][CB];
 #pragma unroll
         for (int rb = 0; rb < LIVE; ++rb) {
-            m_ref[rb] = -1e30f;          // (no token seen yet)
+            m_ref[rb] = kNoTokenSeen;
             l_run[rb] = 0.0f;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -744,7 +747,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                                      : shp.own_partials + (static_cast<int64_t>(seq) * shp.n_kv_heads + kvh) * own_rows * splits;
 #pragma unroll
         for (int rb = 0; rb < LIVE; ++rb) {
-            float m_all = -1e30f;
+            float m_all = kNoTokenSeen;
 #pragma unroll
             for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, sm.ml[w][rb * 16 + n][0]);
             const float weight = exp2_raw(m_ref[rb] - m_all);
@@ -761,7 +764,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 const int64_t prow = prow0 + static_cast<int64_t>(row) * splits + split;
                 *reinterpret_cast<f32x4_t *>(part_acc + prow * D + (e % (D / 4)) * 4) = sum;
                 if (e % (D / 4) == 0) {
-                    float m = -1e30f, l = 0.0f;
+                    float m = kNoTokenSeen, l = 0.0f;
 #pragma unroll
                     for (int w = 0; w < NW; ++w) m = fmaxf(m, sm.ml[w][rb * 16 + r][0]);
 #pragma unroll

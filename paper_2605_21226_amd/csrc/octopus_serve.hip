@@ -49,7 +49,6 @@ __global__ __launch_bounds__(kMergeThreads) void prefix_merge_kernel(PrefixShape
                                                            float *__restrict__ out) {
     typedef float f4_t __attribute__((ext_vector_type(4)));
     constexpr int LANES = D / 4, GROUPS = kMergeThreads / LANES, AHEAD = 16 / GROUPS;
-    constexpr float kNone = -3e38f;              // (below every reference that the attention kernel writes)
     __shared__ __attribute__((aligned(16))) float sums[GROUPS][D];
     __shared__ float ml_of[GROUPS][2];
     const int c = threadIdx.x % LANES, grp = threadIdx.x / LANES;
@@ -69,7 +68,7 @@ __global__ __launch_bounds__(kMergeThreads) void prefix_merge_kernel(PrefixShape
         const int64_t second = s.own_partials + ((static_cast<int64_t>(seq) * s.n_kv_heads + kvh) * s.n_q * hpk + qi * hpk + head % hpk) * s.own_splits - n_shared;
         const int total = n_shared + n_own;
 
-        float m = kNone, l = 0.0f;
+        float m = kNoTokenSeen, l = 0.0f;
         f4_t acc = f4_t{0.0f, 0.0f, 0.0f, 0.0f};
         for (int i0 = grp; i0 < total; i0 += AHEAD * GROUPS) {
             f4_t x[AHEAD];
@@ -103,7 +102,7 @@ __global__ __launch_bounds__(kMergeThreads) void prefix_merge_kernel(PrefixShape
         }
         __syncthreads();
         for (int e = threadIdx.x; e < D; e += kMergeThreads) {
-            float m_all = kNone, l_all = 0.0f, sum = 0.0f;
+            float m_all = kNoTokenSeen, l_all = 0.0f, sum = 0.0f;
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) m_all = fmaxf(m_all, ml_of[g][0]);
 #pragma unroll

@@ -124,7 +124,10 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb, const void *
     s.q = q;
     s.q_is_bf16 = q_dtype == OCTOPUS_DTYPE_BF16 ? 1 : 0;
     s.signs = signs;
-    s.scale = scale;
+    // (the tables' entries are 256 rho n, scores are in units of log2)
+    int exponent = 0;
+    s.scale_part = static_cast<float>(std::frexp(scale * 1.4426950408889634 / (256.0 * std::sqrt(static_cast<double>(cb->plan.head_dim))), &exponent));
+    s.scale_exp = exponent;
     float *part_ml = static_cast<float *>(workspace);
     float *part_acc = reinterpret_cast<float *>(static_cast<char *>(workspace) + up256(partials * 2 * sizeof(float)));
     int err = before != nullptr ? record_event(before, stream) : 0;
