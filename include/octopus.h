@@ -580,6 +580,8 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
  *                block_table and seq_lens are not looked at.
  *   out          device fp32 [n_seq][n_q][n_q_heads][d]; a query that sees no token yields zeros.
  *   workspace    device, 256-byte aligned, at least octopus_attn_prefix_workspace(...) bytes of the same shape; contents are scratch.
+ *                The size does not shrink as n_seq, n_q_heads, n_q, max_prefix or max_len grow: one for a server's largest step serves
+ *                every smaller one.
  * A value that is not a finite number makes its channel no finite number either for the queries that see its token; what a query does
  * not see (tokens past the lengths, later ones for causality) has no say, whatever it is.
  * Any n_q, n_seq and head ratio (all n_seq * n_q * n_q_heads <= 2^26 rows, n_seq * n_q <= 2^24).  octopus_profile_events takes the call.

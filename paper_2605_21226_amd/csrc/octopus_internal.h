@@ -169,9 +169,12 @@ struct PrefixShape {
     int32_t prefix_segments, n_segments;
     int64_t own_partials;   // partial results before the first of a sequence's own (one per query row and range)
 };
-// The division of a call (n_segments 0: no tokens at all) and how many partial results it has at most.
+// The division of a call (n_segments 0: no tokens at all).
 PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
-                              int64_t max_prefix, int64_t max_len, int64_t *partials);
+                              int64_t max_prefix, int64_t max_len);
+// Partial results that the workspace of a call with `rows` query rows (of all sequences and heads) has room for: no fewer than its
+// division makes, and no fewer than for any call with no more rows and no longer contexts.
+int64_t prefix_room(const octopus_plan_t &plan, int64_t rows, int64_t max_prefix, int64_t max_len);
 int launch_prefix(const octopus_codebooks_t &cb, const PrefixShape &s, const void *k_pool, const void *v_pool, const int32_t *prefix_table,
                   const int32_t *prefix_len, const int32_t *block_table, const int32_t *seq_lens, const int32_t *q_lens, float *part_ml,
                   float *part_acc, void *stream);
