@@ -551,7 +551,8 @@ int octopus_append_paged(const octopus_codebooks_t *cb,
  * position if they were when they were encoded) and the value rows of those slots (dequantised where v_bits is 2..4); other rows,
  * and slots past max_pages_per_seq * 64, are left as they were.  Either output may be NULL, and its pool then is not looked at (nor
  * signs without keys).  Other arguments as for octopus_append_paged.
- * Errors: EINVAL (also n_seq or n_kv_heads above 65535, and more than 2^23 (tile, KV head, sequence) triples), EUNSUPPORTED, EHIP. */
+ * Errors: EINVAL (also n_seq or n_kv_heads above 65535, more than 2^23 (tile, KV head, sequence) triples, and at head dimension 256
+ * 2^29 - 128 tokens of a sequence), EUNSUPPORTED, EHIP. */
 int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
                        const void *k_pool, const void *v_pool, int32_t v_bits, int32_t v_group, int32_t n_pages,
                        const int32_t *block_table, int32_t max_pages_per_seq,

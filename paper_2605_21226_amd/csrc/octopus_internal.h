@@ -204,6 +204,9 @@ struct AppendCall {
 int launch_append(const octopus_codebooks_t &cb, const AppendCall &a, void *stream);
 int launch_append_values(const AppendCall &a, int32_t head_dim, int32_t bits, int32_t group, void *vq_pool, void *stream);
 // Reading back (octopus_read.hpp); k_out or v_out may be NULL.
+// (wavefronts a workgroup: at head dimension 256, whose tile in LDS lets two workgroups into a compute unit, twice as many -- 23.1 us
+// with four for five ragged tails of 777 tokens, 16.3 with eight; at 128 eight make no difference)
+constexpr int read_waves(int head_dim) { return head_dim == 256 ? 8 : 4; }
 struct ReadCall {
     const void *k_pool, *v_pool;
     void *k_out, *v_out;

@@ -21,10 +21,6 @@ struct ReadSmem {
     float c_rho[P::NCLASS][kMaxLevels];
 };
 
-// (wavefronts a workgroup: at head dimension 256, whose tile in LDS lets two workgroups into a compute unit, twice as many -- 23.1 us
-// with four for the ragged tails, 16.3 with eight; at 128 eight make no difference)
-constexpr int read_waves(int d) { return d == 256 ? 8 : 4; }
-
 template <class P>
 __global__ __launch_bounds__(read_waves(P::D) * 64) void read_tokens_kernel(DeviceBooks books, ReadCall a) {
     constexpr int D = P::D, NWV = read_waves(D), NT = NWV * 64, LPR = D / 8, RPP = NT / LPR;

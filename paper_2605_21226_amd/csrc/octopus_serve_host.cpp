@@ -233,7 +233,9 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs, cons
     if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(start_pos, 4) || !aligned(lens, 4))
         return OCTOPUS_EINVAL;
     if (start_pos == nullptr && n_tok > static_cast<int64_t>(max_pages_per_seq) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
-    if ((static_cast<int64_t>(n_tok) / 64 + 2) * n_kv_heads * n_seq > (1 << 23)) return OCTOPUS_EINVAL;   // (workgroups of 256 threads)
+    // (workgroups; and a launch counts the threads along its tiles, one more than the tokens fill, in 32 bits)
+    if ((static_cast<int64_t>(n_tok) / 64 + 2) * n_kv_heads * n_seq > (1 << 23)) return OCTOPUS_EINVAL;
+    if (((static_cast<int64_t>(n_tok) + 63) / 64 + 1) * 64 * read_waves(cb->plan.head_dim) > UINT32_MAX) return OCTOPUS_EINVAL;
     if (n_tok == 0) return OCTOPUS_OK;
     ReadCall a{};
     a.k_pool = k_pool;
