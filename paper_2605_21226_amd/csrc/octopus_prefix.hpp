@@ -776,8 +776,8 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
             lds_barrier();
         }
         };
+        static_assert(RB <= 2, "a walk for each count of blocks with rows");
         if (RB == 1 || live == 1) walk(std::integral_constant<int, 1>{});
-        else if (RB == 2 || live == 2) walk(std::integral_constant<int, (RB > 1 ? 2 : 1)>{});
         else walk(std::integral_constant<int, RB>{});
     }
 }
