@@ -497,6 +497,18 @@ def octopus_attn_prefix_workspace(cb, n_seq, n_q_heads, n_kv_heads, n_q, max_pre
                                                     int(max_prefix), int(max_len)))
 
 
+def _check_pools(plan, d, k_pool, v_pool, n_pages, n_kv, v_bits, v_group):
+    """That rows are the plan's and the pools hold the pages that a call may write to or read from; either pool may be None."""
+    assert d == plan.head_dim
+    rows = 64 * n_pages * n_kv
+    assert k_pool is None or k_pool.nbytes >= 16 * rows * plan.granules
+    if v_pool is not None:
+        if v_bits == 0:
+            assert v_pool.nbytes >= 2 * rows * d and _dtype_code(v_pool) == DTYPE_BF16
+        elif v_group in (16, 32):         # (the library refuses other groups)
+            assert v_pool.nbytes >= rows * (v_bits * d // 8 + d // v_group * 8)
+
+
 def octopus_attn_decode_paged_prefix(cb, q, signs, k_pool, v_pool, prefix_table, prefix_len, max_prefix, block_table, seq_lens,
                                      max_len, scale, out, workspace, q_lens=None, causal=False, stream=None):
     """Attention of sequences that share a prefix: q device [n_seq, n_q, n_q_heads, d] contiguous, v_pool device bf16 [n_pages,
@@ -506,7 +518,8 @@ def octopus_attn_decode_paged_prefix(cb, q, signs, k_pool, v_pool, prefix_table,
     assert q.is_contiguous() and v_pool.is_contiguous() and out.is_contiguous()
     n_seq, n_q, n_qh, d = q.shape
     n_pages, n_kv = v_pool.shape[0], v_pool.shape[1]
-    assert tuple(v_pool.shape[2:]) == (64, d) and _dtype_code(v_pool) == DTYPE_BF16
+    assert tuple(v_pool.shape[2:]) == (64, d)
+    _check_pools(cb.plan, d, k_pool, v_pool, n_pages, n_kv, 0, 0)
     assert out.shape == q.shape and _dtype_code(out) == DTYPE_F32
     assert prefix_table is None or prefix_table.is_contiguous()
     assert block_table is None or (block_table.is_contiguous() and block_table.shape[0] == n_seq)
@@ -527,12 +540,12 @@ def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, 
     contiguous channels; k and v of one type), rope device fp32 [n_pos, dim / 2, 2] contiguous (cos, sin) or None, rope_pos device
     int32 [n_seq] or None (the slots), q_out device [n_seq, n_new, n_q_heads, d] contiguous, v_pool device bf16 pages or, with v_bits,
     uint8 rows; start_pos and new_lens device int32 [n_seq] or None."""
-    n_seq, n_new, n_kv, _ = shape = k.shape
+    n_seq, n_new, n_kv, d = shape = k.shape
+    _check_pools(cb.plan, d, k_pool, v_pool, n_pages, n_kv, v_bits, v_group)
     ks, kt, kh, kc = k.stride()
     vs, vt, vh, vc = v.stride()
-    kind = _dtype_code(k)
-    assert kc == 1 and vc == 1 and v.shape == shape and _dtype_code(v) == kind
-    assert block_table.is_contiguous() and block_table.shape[0] == n_seq
+    b_seq, max_pages = block_table.shape
+    assert kc == 1 and vc == 1 and v.shape == shape and v.dtype == k.dtype and block_table.is_contiguous() and b_seq == n_seq
     turn = None
     if rope is not None:
         n_pos, pairs, two = rope.shape
@@ -540,14 +553,14 @@ def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, 
         turn = ctypes.byref(Rope(rope.data_ptr(), n_pos, _ptr(rope_pos), 2 * pairs, 1 if rope_interleaved else 0))
     if q is not None:
         qs, qt, qh, qc = q.stride()
-        q_seq, q_new, n_qh, _ = q.shape
-        assert qc == 1 and q_seq == n_seq and q_new == n_new and q_out.is_contiguous() and q_out.shape == q.shape
+        q_seq, q_new, n_qh, q_d = q_shape = q.shape
+        assert qc == 1 and q_seq == n_seq and q_new == n_new and q_d == d and q_out.is_contiguous() and q_out.shape == q_shape
         q_args = (q.data_ptr(), _dtype_code(q), qs, qt, qh, n_qh, q_out.data_ptr(), _dtype_code(q_out))
     else:
         q_args = _NO_QUERIES
     code = load().octopus_append_paged(
-        ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, kind, n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
-        _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), block_table.shape[1], _ptr(start_pos),
+        ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, _dtype_code(k), n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
+        _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), max_pages, _ptr(start_pos),
         _stream_ptr(stream))
     _check(code, "octopus_append_paged")
 
@@ -557,13 +570,14 @@ def octopus_read_paged(cb, signs, k_pool, v_pool, n_pages, block_table, k_out, v
     """Tokens start_pos[s] + t of a paged cache as values: k_out and v_out device [n_seq, n_tok, n_kv_heads, d] contiguous, of one
     type (either may be None), lens device int32 [n_seq] or None."""
     like = k_out if k_out is not None else v_out
-    n_seq, n_tok, n_kv, _ = like.shape
-    assert block_table.is_contiguous() and block_table.shape[0] == n_seq
-    for t in (k_out, v_out):
-        assert t is None or (t.is_contiguous() and t.shape == like.shape and t.dtype == like.dtype)
+    n_seq, n_tok, n_kv, d = shape = like.shape
+    b_seq, max_pages = block_table.shape
+    assert like.is_contiguous() and block_table.is_contiguous() and b_seq == n_seq
+    _check_pools(cb.plan, d, None if k_out is None else k_pool, None if v_out is None else v_pool, n_pages, n_kv, v_bits, v_group)
+    assert v_out is like or v_out is None or (v_out.is_contiguous() and v_out.shape == shape and v_out.dtype == like.dtype)
     code = load().octopus_read_paged(
-        ctypes.byref(cb), _ptr(signs), _ptr(k_pool), _ptr(v_pool), int(v_bits), int(v_group), int(n_pages), _ptr(block_table),
-        int(block_table.shape[1]), n_seq, n_kv, _ptr(start_pos), n_tok, _ptr(lens), _ptr(k_out), _ptr(v_out), _dtype_code(like),
+        ctypes.byref(cb), _ptr(signs), _ptr(k_pool), _ptr(v_pool), int(v_bits), int(v_group), int(n_pages), block_table.data_ptr(),
+        max_pages, n_seq, n_kv, _ptr(start_pos), n_tok, _ptr(lens), _ptr(k_out), _ptr(v_out), _dtype_code(like),
         _stream_ptr(stream))
     _check(code, "octopus_read_paged")
 
