@@ -1,0 +1,76 @@
+"""The arithmetic of the shared-prefix attention on the CPU, with any of its corrections left out: ordinary inputs, their attention in
+64 bits, and what the kernel's operands make of it.
+
+A key's coordinate is two fp16 numbers, each cut off at 11 bits, a query's two, each rounded to the nearest; the product of the
+remainders is left out.  That is off by at most (2^-20 + 2^-22 + 2^-21) |k_i q_i| < 2^-19 |k_i q_i| a term.  Terms are off in either
+direction, so a score is off by some 2^-19 scale sqrt(sum k_i^2 q_i^2), which is 2^-19 for coordinates of about one, and by the fp32
+sums' roundings (some 30 of 2^-24, in either direction: 2^-21).  Probabilities are two bf16 numbers (2^-18) and an fp32 exponential
+(2^-22); numerator and denominator make twice the score's of it: 2 (2^-19 + 2^-21) + 2^-18 + 2^-22 < 2^-16 of the output's root mean
+square, TOLERANCE."""
+import numpy as np
+
+import oracle
+
+TOLERANCE = 2.0 ** -16
+CASES = [(64, 4), (64, 1.5), (64, 2), (128, 3), (128, 2.5), (128, 4), (128, 1), (256, 2.5), (256, 4), (256, 3)]     # joint tables, two bit widths to a key, none
+N_KV, G, PREFIX, OWN = 2, 8, 300, 70
+
+
+class Inputs:
+    """One KV head of `heads` has keys [tokens, d] as records, values and query rows [G, d]; tokens: the prefix's, then the own ones."""
+
+    def __init__(self, d, bits):
+        rng = np.random.default_rng(10 * d + int(2 * bits))
+        self.d, self.plan, self.scale = d, oracle.make_plan(d, bits), d ** -0.5
+        self.signs = rng.integers(0, 2, size=(N_KV, d)).astype(np.int8) * 2 - 1
+        keys = rng.standard_normal((N_KV, PREFIX + OWN, d))
+        self.rec = np.stack([oracle.encode(self.plan, keys[h], self.signs[h]) for h in range(N_KV)])
+        self.v = (rng.standard_normal((N_KV, PREFIX + OWN, d)).astype(np.float32).view(np.uint32) & 0xFFFF0000).view(np.float32)   # bf16
+        self.q = rng.standard_normal((1, 1, N_KV * G, d)).astype(np.float32)
+
+    def exact(self):
+        out = np.zeros(self.q.shape)
+        for h in range(N_KV):
+            s = self.scale * (self.q[0, 0, h * G:(h + 1) * G].astype(np.float64) @ oracle.reconstruct(self.plan, self.rec[h], self.signs[h]).T)
+            p = np.exp(s - s.max(axis=-1, keepdims=True))
+            out[0, 0, h * G:(h + 1) * G] = p @ self.v[h].astype(np.float64) / p.sum(axis=-1, keepdims=True)
+        return out
+
+
+def off(got, want):
+    return np.sqrt(np.mean((got - want) ** 2) / np.mean(want ** 2))
+
+
+def _cut16(x):
+    """fp16, cut off"""
+    y = x.astype(np.float16)
+    over = np.abs(y.astype(np.float64)) > np.abs(x)
+    return np.where(over, np.nextafter(y, np.float16(0)), y).astype(np.float64)
+
+
+def _bf16(x):
+    u = x.astype(np.float32).view(np.uint32)
+    return ((u + 0x7FFF + ((u >> 16) & 1)) & 0xFFFF0000).view(np.float32).astype(np.float64)
+
+
+def model(x, without=""):
+    """The output of Inputs x with the kernel's operands; without: "key", "query" or "probability", whose second parts are left out."""
+    out = np.zeros(x.q.shape)
+    for h in range(N_KV):
+        k = oracle.reconstruct(x.plan, x.rec[h], x.signs[h])
+        gamma = np.linalg.norm(k, axis=-1, keepdims=True)
+        k = 256.0 * np.stack([oracle.rotate(row, x.signs[h]) for row in k / gamma])
+        q = np.stack([oracle.rotate(row, x.signs[h]) for row in x.q[0, 0, h * G:(h + 1) * G].astype(np.float64)])
+        q_size = 2.0 ** np.ceil(np.log2(np.max(np.abs(q), axis=-1, keepdims=True)))
+        kh, qh = _cut16(k), (q / q_size).astype(np.float16).astype(np.float64)
+        kl, ql = _cut16(k - kh), (q / q_size - qh).astype(np.float16).astype(np.float64)
+        if without == "key":
+            kl = 0 * kl
+        if without == "query":
+            ql = 0 * ql
+        s = (qh @ kh.T + ql @ kh.T + qh @ kl.T) * gamma.T * q_size * (x.scale / 256.0)
+        p = np.exp(s - s.max(axis=-1, keepdims=True))
+        ph = _bf16(p)
+        pl = 0.0 if without == "probability" else _bf16(p - ph)
+        out[0, 0, h * G:(h + 1) * G] = (ph + pl) @ x.v[h].astype(np.float64) / p.sum(axis=-1, keepdims=True)
+    return out
