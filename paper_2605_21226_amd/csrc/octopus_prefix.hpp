@@ -9,7 +9,7 @@
 // which order its terms come, so a lane of group g = lane / 16 decodes the g-th quarter of the triplets of key lane % 16 and puts their
 // coordinates one after the other into the eight places that it has in each operand.  A table by (direction, norm) codes holds
 // (x, y, z, 0) of a triplet as four fp16 numbers and their four remainders, a 16-byte entry; three products -- leading parts, and either
-// one with the other's remainders -- give 22 bits of each factor.  Probabilities are two bf16 numbers each, values are bf16 as they are.
+// one with the other's remainders -- give 22 bits of each factor.  Probabilities are three bf16 numbers each, values are bf16 as they are.
 //
 // No decoded key is written anywhere and no barrier is in the loop: a wavefront owns steps of 32 tokens (its records and value rows
 // staged in LDS of its own) and 32 query rows, 16 at head dimension 256; the wavefronts of a workgroup take the steps of a segment in
@@ -115,12 +115,9 @@ __device__ __forceinline__ uint4 half_triplet(float x, float y, float z) {
     return r;
 }
 
-// Two fp32 numbers as bf16, rounded to the nearest, the first in the lower half.
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-    typedef float f32x2_t __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
-}
+// fp32 numbers as bf16, cut off: one as fp32 again, two in a word, the first in the lower half.
+__device__ __forceinline__ float bf16_cut(float a) { return __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf16_cut_pair(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 
 // Until at most N of the loads from memory asked for are on their way (they arrive in order), and until LDS has answered.
 template <int N>
@@ -474,6 +471,9 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 }
             }
         };
+        // (the next step's are read before the values' products, or, where that spills, behind the last of the channels' reads: 4 bits at
+        // head dimension 128, 64 sequences behind 8192 tokens 101 against 98.9 us, causal drafts 87.5 against 83.4; 1.5 bits 71 against 77)
+        constexpr bool WORDS_LATE = D == 128 && !C::J0;
         if (work) {
             store_records();
             __builtin_amdgcn_wave_barrier();
@@ -617,20 +617,26 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                     for (int cb = 0; cb < CB; ++cb) oacc[rb][cb] *= alpha;
                 }
             }
-            prefix_bf16x8_t p_hi[LIVE], p_lo[LIVE];
+            prefix_bf16x8_t p_hi[LIVE], p_mid[LIVE], p_lo[LIVE];
 #pragma unroll
             for (int rb = 0; rb < LIVE; ++rb) {
-                uint32_t ph[4], pl[4];
+                uint32_t ph[4], pm[4], pl[4];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const float p0 = exp2_raw(fmaf(score[e / 4][rb][e % 4], factor[rb], -m_ref[rb]));
                     const float p1 = exp2_raw(fmaf(score[e / 4][rb][e % 4 + 1], factor[rb], -m_ref[rb]));
                     l_run[rb] += p0 + p1;
-                    // two bf16 numbers, each rounded to the nearest, whose sum is p to 2^-18: the values are bf16
-                    ph[e / 2] = bf16_pair(p0, p1);
-                    pl[e / 2] = bf16_pair(p0 - bf16_lo(ph[e / 2]), p1 - bf16_hi(ph[e / 2]));
+                    // Three bf16 numbers of eight bits each, whose sum is p to its last bit; the values are bf16.  (Two, rounded to the
+                    // nearest, are off by up to 2^-17, and the output by 1.6e-6 to 2.0e-6 of its root mean square, fp32 torch by 0.6e-6 to
+                    // 2.9e-6; three make it 0.3e-6 to 0.5e-6 and cost 1 to 10 %: 64 sequences behind 8192 tokens
+                    // 71 -> 74.5 us, 16 behind 65531 72 -> 78, 32 at d = 256 behind 16384 70 -> 71.5.)
+                    ph[e / 2] = bf16_cut_pair(p0, p1);
+                    const float r0 = p0 - bf16_cut(p0), r1 = p1 - bf16_cut(p1);
+                    pm[e / 2] = bf16_cut_pair(r0, r1);
+                    pl[e / 2] = bf16_cut_pair(r0 - bf16_cut(r0), r1 - bf16_cut(r1));
                 }
                 p_hi[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(ph[0], ph[1], ph[2], ph[3]));
+                p_mid[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pm[0], pm[1], pm[2], pm[3]));
                 p_lo[rb] = __builtin_bit_cast(prefix_bf16x8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
             }
             // nothing reads this step's records any more: the next step's take their place
@@ -638,7 +644,7 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 __builtin_amdgcn_wave_barrier();
                 store_records();
                 __builtin_amdgcn_wave_barrier();
-                read_words();
+                if (!WORDS_LATE) read_words();
             }
             // The values have arrived. Rows past the last token are made zeros: their probabilities are zero, but what lies there may
             // be no number.
@@ -708,9 +714,12 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
                 if (cb + AHEAD_V - 1 < CB) ask_values(cb + AHEAD_V - 1);
+                if (WORDS_LATE && cb + AHEAD_V - 1 == CB && more) read_words();
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_hi[rb], oacc[rb][cb], 0, 0, 0);
+#pragma unroll
+                for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_mid[rb], oacc[rb][cb], 0, 0, 0);
 #pragma unroll
                 for (int rb = 0; rb < LIVE; ++rb) oacc[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[cb % AHEAD_V].b, p_lo[rb], oacc[rb][cb], 0, 0, 0);
             }

@@ -2,16 +2,17 @@
 64 bits, and what the kernel's operands make of it.
 
 A key's coordinate is two fp16 numbers, each cut off at 11 bits, a query's two, each rounded to the nearest; the product of the
-remainders is left out.  That is off by at most (2^-20 + 2^-22 + 2^-21) |k_i q_i| < 2^-19 |k_i q_i| a term.  Terms are off in either
-direction, so a score is off by some 2^-19 scale sqrt(sum k_i^2 q_i^2), which is 2^-19 for coordinates of about one, and by the fp32
-sums' roundings (some 30 of 2^-24, in either direction: 2^-21).  Probabilities are two bf16 numbers (2^-18) and an fp32 exponential
-(2^-22); numerator and denominator make twice the score's of it: 2 (2^-19 + 2^-21) + 2^-18 + 2^-22 < 2^-16 of the output's root mean
-square, TOLERANCE."""
+remainders is left out.  In the root mean square a term k_i q_i is off by no more than 2^-10 2^-10 / 3 of it for the key's last bits
+(a remainder below 2^-10, cut off below 2^-10 of itself, both spread evenly), 2^-11 2^-11 / 3 for the query's and 2^-10 2^-11 / 3 for the
+product left out: 2^-21 together, in any direction.  For coordinates of about one, scale sqrt(sum k_i^2 q_i^2) is one and so a score is
+off by 2^-21.  Its fp32 sums round some 30 times, by 2^-25 of sums of two or three: 2^-22 together.  Probabilities are three bf16 numbers
+that make the fp32 one exactly, and that is an exponential's (2^-23); sums of them round by 2^-23 again.  Numerator and denominator
+take twice the score's part: 2 (2^-21 + 2^-22) + 2 2^-23 < 2^-19 of the output's root mean square, TOLERANCE."""
 import numpy as np
 
 import oracle
 
-TOLERANCE = 2.0 ** -16
+TOLERANCE = 2.0 ** -19
 CASES = [(64, 4), (64, 1.5), (64, 2), (128, 3), (128, 2.5), (128, 4), (128, 1), (256, 2.5), (256, 4), (256, 3)]     # joint tables, two bit widths to a key, none
 N_KV, G, PREFIX, OWN = 2, 8, 300, 70
 
@@ -48,13 +49,13 @@ def _cut16(x):
     return np.where(over, np.nextafter(y, np.float16(0)), y).astype(np.float64)
 
 
-def _bf16(x):
-    u = x.astype(np.float32).view(np.uint32)
-    return ((u + 0x7FFF + ((u >> 16) & 1)) & 0xFFFF0000).view(np.float32).astype(np.float64)
+def _cut_bf16(x):
+    return (x.astype(np.float32).view(np.uint32) & 0xFFFF0000).view(np.float32).astype(np.float64)
 
 
 def model(x, without=""):
-    """The output of Inputs x with the kernel's operands; without: "key", "query" or "probability", whose second parts are left out."""
+    """The output of Inputs x with the kernel's operands; without: "key" or "query", whose remainders are left out, or "middle" or
+    "last", a part of the probabilities."""
     out = np.zeros(x.q.shape)
     for h in range(N_KV):
         k = oracle.reconstruct(x.plan, x.rec[h], x.signs[h])
@@ -69,8 +70,11 @@ def model(x, without=""):
         if without == "query":
             ql = 0 * ql
         s = (qh @ kh.T + ql @ kh.T + qh @ kl.T) * gamma.T * q_size * (x.scale / 256.0)
-        p = np.exp(s - s.max(axis=-1, keepdims=True))
-        ph = _bf16(p)
-        pl = 0.0 if without == "probability" else _bf16(p - ph)
-        out[0, 0, h * G:(h + 1) * G] = (ph + pl) @ x.v[h].astype(np.float64) / p.sum(axis=-1, keepdims=True)
+        p = np.exp(s - s.max(axis=-1, keepdims=True)).astype(np.float32).astype(np.float64)
+        first = _cut_bf16(p)
+        middle = _cut_bf16(p - first)
+        last = _cut_bf16(p - first - middle)
+        assert np.array_equal(first + middle + last, p)
+        parts = first + (0.0 if without == "middle" else middle) + (0.0 if without == "last" else last)
+        out[0, 0, h * G:(h + 1) * G] = parts @ x.v[h].astype(np.float64) / p.sum(axis=-1, keepdims=True)
     return out
