@@ -100,11 +100,13 @@ struct PrefixSmem {
     float c_rho[P::NCLASS][1 << (P::BN0 > P::BN1 ? P::BN0 : P::BN1)];
 };
 
-// 256 (x, y, z, 0) as fp16 and the remainders as fp16: together 22 bits of each (a product drops the remainders' product only).
+// 256 (x, y, z, 0) as fp16 and the remainders as fp16, each rounded to the nearest: together 22 bits of each (a product drops the
+// remainders' product only).
 __device__ __forceinline__ uint4 half_triplet(float x, float y, float z) {
     auto two = [](float a, float b) {
-        const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-        return __builtin_bit_cast(uint32_t, h);
+        typedef float f32x2_t __attribute__((ext_vector_type(2)));
+        typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), half2_t));
     };
     auto lower = [](uint32_t w) { return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(w))); };
     uint4 r;
@@ -488,6 +490,12 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
         for (int step = begin + wave; step < end; step += NW) {
             const bool more = step + NW < end, two_more = step + 2 * NW < end;
             f32x4_t score[2][LIVE];      // [key block][row block]: lane (n, g) has keys 4 g .. + 3 of row n
+            // The remainders' products have sums of their own where registers are left for them: a sum that is already large takes off
+            // their last bits (4 beams of 4 rows behind 700 tokens: the output off by 0.62e-6 of its root mean square instead of 0.86e-6,
+            // fp32 torch 0.72e-6; at d = 64 two row blocks 0.76e-6 instead of 1.15e-6; 1 % of the time).  With two row blocks at d = 128 they spill
+            // (16 sequences behind 65531 tokens: 78 -> 100 us) and the error, 1.3e-6 over a long prefix, is below fp32 torch's 2.1e-6 as it is.
+            constexpr bool APART = LIVE == 1 || D == 64;
+            f32x4_t rest[2][LIVE];
             float gamma[2][4];
             // An operand of a key block at a time; the entries of the next one (triplets that begin there) are asked for before the
             // products of this one, as LDS takes longer to answer than a product.
@@ -571,20 +579,25 @@ __global__ __launch_bounds__(PrefixCfg<P>::NT) __attribute__((amdgpu_waves_per_e
                 });
                 // (each of these loops has products that do not wait for each other)
                 constexpr int first = s / KS;
+                const f32x4_t zero = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int e = 0; e < NB * LIVE; ++e)
-                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], qh[e % LIVE][kk], kk == 0 ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : score[first + e / LIVE][e % LIVE], 0, 0, 0);
+                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], qh[e % LIVE][kk], kk == 0 ? zero : score[first + e / LIVE][e % LIVE], 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < NB * LIVE; ++e)
-                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], ql[e % LIVE][kk], score[first + e / LIVE][e % LIVE], 0, 0, 0);
+                for (int e = 0; e < NB * LIVE; ++e) {
+                    f32x4_t &to = APART ? rest[first + e / LIVE][e % LIVE] : score[first + e / LIVE][e % LIVE];
+                    to = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[e / LIVE], ql[e % LIVE][kk], APART && kk == 0 ? zero : to, 0, 0, 0);
+                }
 #pragma unroll
-                for (int e = 0; e < NB * LIVE; ++e)
-                    score[first + e / LIVE][e % LIVE] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl[e / LIVE], qh[e % LIVE][kk], score[first + e / LIVE][e % LIVE], 0, 0, 0);
+                for (int e = 0; e < NB * LIVE; ++e) {
+                    f32x4_t &to = APART ? rest[first + e / LIVE][e % LIVE] : score[first + e / LIVE][e % LIVE];
+                    to = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl[e / LIVE], qh[e % LIVE][kk], to, 0, 0, 0);
+                }
             });
 #pragma unroll
             for (int rb = 0; rb < LIVE; ++rb)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) score[e / 4][rb][e % 4] *= gamma[e / 4][e % 4];
+                for (int e = 0; e < 8; ++e) score[e / 4][rb][e % 4] = (APART ? score[e / 4][rb][e % 4] + rest[e / 4][rb][e % 4] : score[e / 4][rb][e % 4]) * gamma[e / 4][e % 4];
             // tokens past the sequence's end, or that a row does not see for causality
             if ((step + 1) * kPrefixKeys > all_see) {
 #pragma unroll

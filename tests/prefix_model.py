@@ -1,13 +1,13 @@
 """The arithmetic of the shared-prefix attention on the CPU, with any of its corrections left out: ordinary inputs, their attention in
 64 bits, and what the kernel's operands make of it.
 
-A key's coordinate is two fp16 numbers, each cut off at 11 bits, a query's two, each rounded to the nearest; the product of the
-remainders is left out.  In the root mean square a term k_i q_i is off by no more than 2^-10 2^-10 / 3 of it for the key's last bits
-(a remainder below 2^-10, cut off below 2^-10 of itself, both spread evenly), 2^-11 2^-11 / 3 for the query's and 2^-10 2^-11 / 3 for the
-product left out: 2^-21 together, in any direction.  For coordinates of about one, scale sqrt(sum k_i^2 q_i^2) is one and so a score is
-off by 2^-21.  Its fp32 sums round some 30 times, by 2^-25 of sums of two or three: 2^-22 together.  Probabilities are three bf16 numbers
-that make the fp32 one exactly, and that is an exponential's (2^-23); sums of them round by 2^-23 again.  Numerator and denominator
-take twice the score's part: 2 (2^-21 + 2^-22) + 2 2^-23 < 2^-19 of the output's root mean square, TOLERANCE."""
+Coordinates of keys and queries are two fp16 numbers each, rounded to the nearest; the product of the remainders is left out.  In the
+root mean square a term k_i q_i is off by no more than 2^-11 2^-11 / 3 of it for either factor's last bits (a remainder below 2^-11,
+rounded by less than 2^-11 of itself, both spread evenly) and as much for the product left out: 2^-22 together, in any direction.
+For coordinates of about one, scale sqrt(sum k_i^2 q_i^2) is one and so a score is off by 2^-22. Its fp32 sums round some 30
+times, by 2^-25 of sums of two or three: 2^-22 together. Probabilities are three bf16 numbers that make the fp32 one exactly, and
+that is an exponential's (2^-23); sums of them round by 2^-23 again. Numerator and denominator take twice the score's part: 2
+(2^-22 + 2^-22) + 2 2^-23 < 2^-19 of the output's root mean square, TOLERANCE."""
 import numpy as np
 
 import oracle
@@ -42,11 +42,8 @@ def off(got, want):
     return np.sqrt(np.mean((got - want) ** 2) / np.mean(want ** 2))
 
 
-def _cut16(x):
-    """fp16, cut off"""
-    y = x.astype(np.float16)
-    over = np.abs(y.astype(np.float64)) > np.abs(x)
-    return np.where(over, np.nextafter(y, np.float16(0)), y).astype(np.float64)
+def _fp16(x):
+    return x.astype(np.float16).astype(np.float64)
 
 
 def _cut_bf16(x):
@@ -63,8 +60,8 @@ def model(x, without=""):
         k = 256.0 * np.stack([oracle.rotate(row, x.signs[h]) for row in k / gamma])
         q = np.stack([oracle.rotate(row, x.signs[h]) for row in x.q[0, 0, h * G:(h + 1) * G].astype(np.float64)])
         q_size = 2.0 ** np.ceil(np.log2(np.max(np.abs(q), axis=-1, keepdims=True)))
-        kh, qh = _cut16(k), (q / q_size).astype(np.float16).astype(np.float64)
-        kl, ql = _cut16(k - kh), (q / q_size - qh).astype(np.float16).astype(np.float64)
+        kh, qh = _fp16(k), _fp16(q / q_size)
+        kl, ql = _fp16(k - kh), _fp16(q / q_size - qh)
         if without == "key":
             kl = 0 * kl
         if without == "query":
