@@ -573,7 +573,8 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
  *                looked at and their rows of out stay as they were.
  *   causal       0: every query sees all own tokens; 1: query i of sequence s sees the prefix and its own tokens
  *                t <= seq_lens[s] - q_lens[s] + i (the queries are those of the last q_lens[s] tokens; none where that is negative).
- *   k_pool, v_pool, n_pages, signs   as for octopus_attn_decode_paged (bf16 values).
+ *   k_pool, v_pool, n_pages, signs   as for octopus_attn_decode_paged (bf16 values; pages of quantised values, the QJL residual and
+ *                windows of recent tokens have the other octopus_attn_decode_paged forms only).
  *   prefix_table device int32 [prefix_pages]: the page of the prefix's tokens 64 j .. 64 j + 63; ids clamped to the pool.
  *   prefix_len   device int32 [1], 0 <= prefix_len <= max_prefix (clamped); max_prefix <= prefix_pages * 64, on the host, sizes the
  *                launch.  max_prefix 0: no prefix; prefix_table and prefix_len are not looked at.
@@ -583,8 +584,8 @@ int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs,
  *   workspace    device, 256-byte aligned, at least octopus_attn_prefix_workspace(...) bytes of the same shape; contents are scratch.
  *                The size does not shrink as n_seq, n_q_heads, n_q, max_prefix or max_len grow: one for a server's largest step serves
  *                every smaller one.
- * A value that is not a finite number makes its channel no finite number either for the queries that see its token; what a query does
- * not see (tokens past the lengths, later ones for causality) has no say, whatever it is.
+ * Scores may be of any size that fp32 holds.  A value that is not a finite number makes its channel no finite number either for the
+ * queries that see its token; what a query does not see (tokens past the lengths, later ones for causality) has no say, whatever it is.
  * Any n_q, n_seq and head ratio (all n_seq * n_q * n_q_heads <= 2^26 rows, n_seq * n_q <= 2^24).  octopus_profile_events takes the call.
  * Errors: EINVAL, EUNSUPPORTED (a plan or type without a kernel; the App. D pairs have none), EWORKSPACE, EHIP. */
 size_t octopus_attn_prefix_workspace(const octopus_codebooks_t *cb, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads,

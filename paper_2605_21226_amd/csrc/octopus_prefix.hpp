@@ -18,9 +18,8 @@
 //
 // What bounds it: the vector units, the matrix cores and LDS, in turns, with two wavefronts a SIMD to hide one behind the other (the
 // accumulators and the queries' operands leave room for no third).  16 sequences of 32 heads behind 65531 tokens with 512 own ones, d = 128,
-// 3 bits: 189 MB in 69 us (2.7 TB/s; at a copy's rate it would be 38), vector units active 51 % of it, matrix cores 36 %, LDS 41 %.  A step of
-// 32 tokens and 32 rows is 92 matrix instructions (1470 clocks) and some 260 vector ones (1040).  A
-// form of 77 us took 70 without memory (one page for all), 76 with table reads that never meet on a bank, 64 with both.
+// 3 bits: 186 MB in 75 us (2.5 TB/s; at a plain read's rate, 7.07, it would be 26), vector units active 52 % of it, matrix cores 39 %, LDS
+// 38 %.  A step of 32 tokens and 32 rows is 108 matrix instructions (1730 clocks) and some 440 vector ones (1760).
 #ifndef OCTOPUS_PREFIX_HPP_
 #define OCTOPUS_PREFIX_HPP_
 

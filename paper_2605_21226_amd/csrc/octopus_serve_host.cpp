@@ -54,7 +54,10 @@ int64_t prefix_room(const octopus_plan_t &plan, int64_t rows, int64_t max_prefix
 
 // Ranges of tokens: a workgroup's segment takes rounds of one step per wavefront and a start of its own (queries, results), the
 // workgroups run in rounds of 256, and every range writes a partial result per query row that the merge reads again.  The number of
-// rounds a segment has at most is the one that makes the least of all that.
+// rounds a segment has at most is, of those tried (each a sixteenth above the one before), the one that makes the least of all that.
+// The two constants are flat: of 13 shapes (one to 200 sequences, 1 to 70 000 tokens, every head dimension) a start of 1.25 rounds instead
+// of 2.5 made one slower, by 3 %, and 5 none; 5e-6 a partial result made none slower, 8e-5 one, by 3 %.  Without a start four took 1.1
+// to 2 times as long.
 PrefixShape make_prefix_shape(const octopus_plan_t &plan, int32_t n_seq, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_q,
                               int64_t max_prefix, int64_t max_len) {
     PrefixShape s{};
