@@ -18,7 +18,7 @@ N_KV, G, PREFIX, OWN = 2, 8, 300, 70
 
 
 class Inputs:
-    """One KV head of `heads` has keys [tokens, d] as records, values and query rows [G, d]; tokens: the prefix's, then the own ones."""
+    """Keys as records [kv, tokens, bytes], values [kv, tokens, d] and queries [1, 1, heads, d]; the prefix's tokens, then the own ones."""
 
     def __init__(self, d, bits):
         rng = np.random.default_rng(10 * d + int(2 * bits))
