@@ -15,8 +15,9 @@
  *   octopus_encode_values_paged, octopus_attn_decode_paged_vq,
  *   octopus_encode_qjl_paged, octopus_attn_decode_paged_qjl
  *                                                  the same codec and attention over a paged cache
- *   octopus_append_paged, octopus_read_paged       a step's keys, values and queries, rotated by position, into pages;
- *                                                  tokens of pages as values again
+ *   octopus_append_paged, octopus_append_paged_axes, octopus_read_paged
+ *                                                  a step's keys, values and queries, rotated by position (on one axis or
+ *                                                  several), into pages; tokens of pages as values again
  *   octopus_attn_decode_paged_prefix               attention of sequences that share a prefix
  *
  * Conventions
@@ -544,6 +545,42 @@ int octopus_append_paged(const octopus_codebooks_t *cb,
                          const int32_t *block_table, int32_t max_pages_per_seq,
                          const int32_t *start_pos,
                          void *stream);
+
+/* ---- appending to pages, with positions on several axes ----
+ * octopus_append_paged for tokens that have a position on each of several axes: frame, row and column of an image's or a video's patches
+ * (text has the same one on all of them).  Pair i goes by the axis that the caller's map gives it, whatever the map: a run of pairs an
+ * axis, or the axes in turns.
+ *   rope         host, not NULL.  (cos, sin) = table[p][i] with p the token's position on axis axis[i]; table, n_pos, dim and interleaved as
+ *                in octopus_rope_t, positions outside [0, n_pos) read as the nearest inside.
+ *                pos: device int32, 4-byte aligned; axis k of new token t of sequence s at pos[s*stride_seq + t*stride_tok + k*stride_axis],
+ *                strides in elements, >= 0 (0: the same for all).  Tokens from new_lens[s] on are not looked at.
+ *                axis: host [dim / 2] bytes, each below n_axes (1 .. OCTOPUS_MAX_AXES); read before the call returns.
+ * With one axis, or the same position on all of them, every byte is that of octopus_append_paged.  Other arguments, launches and errors as there; EINVAL
+ * also for rope NULL, pos or axis NULL, an axis past the last one, a negative stride. */
+#define OCTOPUS_MAX_AXES 4
+typedef struct octopus_rope_axes {
+    const float *table;
+    int64_t n_pos;
+    const int32_t *pos;
+    int64_t stride_seq, stride_tok, stride_axis;
+    const uint8_t *axis;
+    int32_t n_axes;
+    int32_t dim;
+    int32_t interleaved;
+} octopus_rope_axes_t;
+
+int octopus_append_paged_axes(const octopus_codebooks_t *cb,
+                              const void *k, int64_t k_stride_seq, int64_t k_stride_tok, int64_t k_stride_head,
+                              const void *v, int64_t v_stride_seq, int64_t v_stride_tok, int64_t v_stride_head, int32_t kv_dtype,
+                              int32_t n_seq, int32_t n_kv_heads, int32_t n_new, const int32_t *new_lens,
+                              const octopus_rope_axes_t *rope,
+                              const void *q, int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head,
+                              int32_t n_q_heads, void *q_out, int32_t q_out_dtype,
+                              const uint8_t *signs,
+                              void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group, int32_t n_pages,
+                              const int32_t *block_table, int32_t max_pages_per_seq,
+                              const int32_t *start_pos,
+                              void *stream);
 
 /* ---- reading tokens of a paged cache back as values ----
  * Rows t < lens[s] (clamped to 0 .. n_tok; NULL: all n_tok) of k_out and v_out, [n_seq][n_tok][n_kv_heads][d] contiguous, out_dtype

@@ -28,7 +28,7 @@ EXPORTS = ("octopus_build_codebooks", "octopus_build_codebooks_pair", "octopus_c
            "octopus_encode_qjl_paged", "octopus_attn_decode_paged_qjl",
            "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores",
            "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix",
-           "octopus_append_paged", "octopus_read_paged")
+           "octopus_append_paged", "octopus_append_paged_axes", "octopus_read_paged")
 
 
 class Plan(ctypes.Structure):
@@ -61,6 +61,21 @@ class Rope(ctypes.Structure):
         ("table", ctypes.c_void_p),
         ("n_pos", ctypes.c_int64),
         ("pos", ctypes.c_void_p),
+        ("dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+    ]
+
+
+class RopeAxes(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("n_pos", ctypes.c_int64),
+        ("pos", ctypes.c_void_p),
+        ("stride_seq", ctypes.c_int64),
+        ("stride_tok", ctypes.c_int64),
+        ("stride_axis", ctypes.c_int64),
+        ("axis", ctypes.c_char_p),
+        ("n_axes", ctypes.c_int32),
         ("dim", ctypes.c_int32),
         ("interleaved", ctypes.c_int32),
     ]
@@ -155,6 +170,8 @@ def load():
     lib.octopus_append_paged.argtypes = [CB, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, i32, i32, vp, ctypes.POINTER(Rope), vp, i32,
                                          i64, i64, i64, i32, vp, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp]
     lib.octopus_append_paged.restype = ctypes.c_int
+    lib.octopus_append_paged_axes.argtypes = [ctypes.POINTER(RopeAxes) if t is ctypes.POINTER(Rope) else t for t in lib.octopus_append_paged.argtypes]
+    lib.octopus_append_paged_axes.restype = ctypes.c_int
     lib.octopus_read_paged.argtypes = [CB, vp, vp, vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, vp, vp, vp, i32, vp]
     lib.octopus_read_paged.restype = ctypes.c_int
     lib.octopus_vq_on_matrix_cores.argtypes = [ctypes.POINTER(Codebooks), i32, i32, i32, i32, i32]
@@ -200,7 +217,7 @@ def octopus_cache_bytes(cb, n_seq, n_kv_heads, t_capacity):
 # imports inside functions and a c_void_p object per argument most of the rest: an encode call 11.8 -> 7.8 us, a decode call of one
 # launch 11.7 -> 7.4.
 _DTYPES = {}
-_raw_stream = _device = None
+_raw_stream = _device = _int32 = None
 
 
 def _dtype_code(t):
@@ -212,6 +229,14 @@ def _dtype_code(t):
             raise TypeError(f"unsupported dtype {t.dtype}")
         code = _DTYPES[t.dtype]
     return code
+
+
+def _is_int32(t):
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    return t.dtype is _int32
 
 
 def _stream_ptr(stream):
@@ -540,17 +565,37 @@ def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, 
     contiguous channels; k and v of one type), rope device fp32 [n_pos, dim / 2, 2] contiguous (cos, sin) or None, rope_pos device
     int32 [n_seq] or None (the slots), q_out device [n_seq, n_new, n_q_heads, d] contiguous, v_pool device bf16 pages or, with v_bits,
     uint8 rows; start_pos and new_lens device int32 [n_seq] or None."""
+    turn = None
+    if rope is not None:
+        n_pos, pairs, two = rope.shape
+        assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
+        turn = ctypes.byref(Rope(rope.data_ptr(), n_pos, _ptr(rope_pos), 2 * pairs, 1 if rope_interleaved else 0))
+    _append("octopus_append_paged", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
+            v_group, stream)
+
+
+def octopus_append_paged_axes(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, rope, rope_axis, rope_pos, start_pos=None,
+                              new_lens=None, rope_interleaved=False, q=None, q_out=None, v_bits=0, v_group=0, stream=None):
+    """octopus_append_paged by positions on several axes: rope device fp32 [n_pos, dim / 2, 2] contiguous, rope_axis the axis of each of the
+    dim / 2 pairs (bytes, or anything that bytes() takes), rope_pos device int32 [n_seq, n_new, n_axes] of any strides."""
+    n_pos, pairs, two = rope.shape
+    assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
+    axis = rope_axis if type(rope_axis) is bytes else bytes(rope_axis)
+    p_seq, p_new, n_axes = rope_pos.shape
+    assert len(axis) == pairs and p_seq == k.shape[0] and p_new == k.shape[1] and _is_int32(rope_pos)
+    turn = ctypes.byref(RopeAxes(rope.data_ptr(), n_pos, rope_pos.data_ptr(), *rope_pos.stride(), axis, n_axes, 2 * pairs,
+                                 1 if rope_interleaved else 0))
+    _append("octopus_append_paged_axes", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
+            v_group, stream)
+
+
+def _append(name, cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits, v_group, stream):
     n_seq, n_new, n_kv, d = shape = k.shape
     _check_pools(cb.plan, d, k_pool, v_pool, n_pages, n_kv, v_bits, v_group)
     ks, kt, kh, kc = k.stride()
     vs, vt, vh, vc = v.stride()
     b_seq, max_pages = block_table.shape
     assert kc == 1 and vc == 1 and v.shape == shape and v.dtype == k.dtype and block_table.is_contiguous() and b_seq == n_seq
-    turn = None
-    if rope is not None:
-        n_pos, pairs, two = rope.shape
-        assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
-        turn = ctypes.byref(Rope(rope.data_ptr(), n_pos, _ptr(rope_pos), 2 * pairs, 1 if rope_interleaved else 0))
     if q is not None:
         qs, qt, qh, qc = q.stride()
         q_seq, q_new, n_qh, q_d = q_shape = q.shape
@@ -558,11 +603,11 @@ def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, 
         q_args = (q.data_ptr(), _dtype_code(q), qs, qt, qh, n_qh, q_out.data_ptr(), _dtype_code(q_out))
     else:
         q_args = _NO_QUERIES
-    code = load().octopus_append_paged(
+    code = getattr(load(), name)(
         ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, _dtype_code(k), n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
         _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), max_pages, _ptr(start_pos),
         _stream_ptr(stream))
-    _check(code, "octopus_append_paged")
+    _check(code, name)
 
 
 def octopus_read_paged(cb, signs, k_pool, v_pool, n_pages, block_table, k_out, v_out, start_pos=None, lens=None, v_bits=0, v_group=0,

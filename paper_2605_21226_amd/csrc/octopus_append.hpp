@@ -5,6 +5,8 @@
 //     a' = a cos - b sin,   b' = a sin + b cos,
 // pairs being channels i and i + dim / 2, or 2 i and 2 i + 1, i < dim / 2; channels from dim on stay.  It is applied in fp32 to the
 // key that the encoder takes: what octopus_encode_paged computes of rotated keys, without their rounding to bf16 in between.
+// A token of an image or a video has a position on each of several axes (frame, row, column), and pair i goes by the one that the
+// caller's map gives it: (cos, sin) = table[p_axis(i)][i].  Those kernels (append_*_axes_kernel) differ in nothing else.
 //
 // What bounds it: memory, for long prompts -- queries, keys and values come and go once, the records are a quarter of the keys -- and
 // latency for a few tokens.  Measured at d = 128, 3 bits, 32 query and 8 KV heads, bf16: 15877 tokens, 366 MB, in 97 us, 3.8 TB/s
@@ -66,6 +68,31 @@ struct RowRotation {
             cs[j + 1] = make_float2(two.z, two.w);
         }
     }
+    // ... of a token's positions on several axes, at p[0], p[stride], ...
+    template <int WORDS>
+    __device__ __forceinline__ void load(const RopeCall &r, const AxesCall &x, const int32_t *p, int col) {
+        half = col < r.dim ? r.dim / 2 : 0;
+        pairs = r.interleaved != 0;
+        upper = col >= half;
+        if (half == 0) return;
+        const int first = pairs ? col / 2 : (upper ? col - half : col);
+        uint32_t axes = x.axis_of[0];            // two bits a pair, 16 pairs a word
+#pragma unroll
+        for (int w = 1; w < WORDS; ++w) axes = first / 16 == w ? x.axis_of[w] : axes;
+        axes >>= 2 * (first % 16);
+        const float2 *row[kMaxAxes];
+#pragma unroll
+        for (int k = 0; k < kMaxAxes; ++k) {     // (axes past the last: the last again)
+            const int64_t pos = p[min(k, x.n_axes - 1) * x.stride_axis];
+            row[k] = reinterpret_cast<const float2 *>(r.table) + min(max(pos, static_cast<int64_t>(0)), r.n_pos - 1) * half + first;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j >= 4 && pairs) break;
+            const uint32_t k = (axes >> (2 * j)) & 3u;
+            cs[j] = (k & 2u ? (k & 1u ? row[3] : row[2]) : (k & 1u ? row[1] : row[0]))[j];
+        }
+    }
     // (all lanes of a row call this: the partners' channels come from other lanes.  One rounding order, whatever the caller: a key has
     // the same codes in a prompt and by itself)
     __device__ __forceinline__ void apply(float (&x)[8], int lane) const {
@@ -101,10 +128,38 @@ __device__ __forceinline__ int64_t append_page(const AppendCall &a, int seq, int
     return min(max(a.pt.table[static_cast<int64_t>(seq) * a.pt.stride + tile], 0), a.pt.n_pages - 1);
 }
 
+// Where a token's rotation comes from: one position, or one on each axis.
+struct OneAxis {
+    struct Sequence {
+        int64_t pos0;      // the position of slot 0, if it were there
+        template <int LPR>
+        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, int64_t slot, int col) const { rot.load(a.rope, pos0 + slot, col); }
+    };
+    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start) const { return {append_position(a, seq, start) - start}; }
+};
+struct ManyAxes {
+    AxesCall x;
+    struct Sequence {
+        const AxesCall &x;
+        const int32_t *pos;
+        int64_t start;
+        int count;         // tokens that have positions, 1 at least
+        template <int LPR>
+        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, int64_t slot, int col) const {
+            // (a tile's slots in front of the first token and behind the last one ask as well, and get the nearest token's)
+            const int64_t tok = min(max(slot - start, static_cast<int64_t>(0)), static_cast<int64_t>(count) - 1);
+            rot.template load<LPR / 4>(a.rope, x, pos + tok * x.stride_tok, col);
+        }
+    };
+    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start) const {
+        return {x, x.pos + seq * x.stride_seq, start, append_count(a, seq)};
+    }
+};
+
 // Few tokens (a decode step appends one per sequence): a wavefront per (token, KV head), which takes the key, the value and the
 // head's queries as rows side by side, eight channels a lane, and encodes the key a triplet per lane.
-template <class P>
-__global__ __launch_bounds__(kWave) void append_token_kernel(DeviceBooks books, AppendCall a) {
+template <class P, class Turn>
+__device__ __forceinline__ void append_token(const AppendCall &a, const Turn &turn) {
     constexpr int D = P::D, LPR = D / 8, ROWS = kWave / LPR;
     constexpr int NX = P::BD0 > 2 || P::BD1 > 2 ? 1 << (P::BD0 > P::BD1 ? P::BD0 : P::BD1) : 4;
     constexpr int NR = 1 << (P::BN0 > P::BN1 ? P::BN0 : P::BN1);
@@ -119,7 +174,7 @@ __global__ __launch_bounds__(kWave) void append_token_kernel(DeviceBooks books, 
     const bool reached = slot < static_cast<int64_t>(a.pt.stride) * kWave;
     const int64_t tile = reached ? (append_page(a, seq, slot / kWave) * a.n_kv_heads + kvh) : 0;
     RowRotation<LPR> rot;
-    rot.load(a.rope, append_position(a, seq, start) + tok, col);
+    turn.of(a, seq, start).load(rot, a, slot, col);
 
     const int hpk = a.q != nullptr ? a.n_q_heads / a.n_kv_heads : 0;
     float key[8];
@@ -209,6 +264,11 @@ __global__ __launch_bounds__(kWave) void append_token_kernel(DeviceBooks books, 
             make_uint4(rec[4 * lane], rec[4 * lane + 1], rec[4 * lane + 2], rec[4 * lane + 3]);
 }
 
+template <class P>
+__global__ __launch_bounds__(kWave) void append_token_kernel(DeviceBooks books, AppendCall a) { append_token<P>(a, OneAxis{}); }
+template <class P>
+__global__ __launch_bounds__(kWave) void append_token_axes_kernel(DeviceBooks books, AppendCall a, ManyAxes turn) { append_token<P>(a, turn); }
+
 // Prompts.  Some workgroups encode: a run of 64-token tiles of one (sequence, KV head), eight coordinates a thread while the keys are
 // loaded and rotated, a key per lane from the transform on (the phases of encode_kernel, with four candidates per triplet).  The
 // others take rows that are not encoded, queries and bf16 values, eight channels a thread and the rows of its token one after the
@@ -217,10 +277,9 @@ __global__ __launch_bounds__(kWave) void append_token_kernel(DeviceBooks books, 
 constexpr int kAppendRows = 8;       // rows of a token per workgroup of the second kind
 constexpr int kAhead = 4;            // of them asked for at once
 
-template <class P>
-__global__ __launch_bounds__(encode_threads<P>())
-__attribute__((amdgpu_waves_per_eu(encode_waves_per_simd<P, false, true>(), encode_waves_per_simd<P, false, true>())))
-void append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int32_t tile_runs, int32_t tiles_per_group, int32_t every) {
+template <class P, class Turn>
+__device__ __forceinline__ void append_tile(const AppendCall &a, const Turn &turn, int32_t key_blocks, int32_t tile_runs, int32_t tiles_per_group,
+                                            int32_t every) {
     constexpr int D = P::D, LPR = D / 8;
     constexpr int NWV = encode_waves<P>(), NT = encode_threads<P>(), RPP = NT / LPR, NPASS = kWave / RPP;
     using Smem = EncodeSmem<P, false, true>;
@@ -258,7 +317,7 @@ void append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int
         }
         if (last > values) {
             RowRotation<LPR> rot;
-            rot.load(a.rope, append_position(a, seq, start) + tok, col);
+            turn.of(a, seq, start).load(rot, a, slot, col);
             const int64_t out = (static_cast<int64_t>(seq) * a.n_new + tok) * a.n_q_heads;
             for (int h0 = max(first - values, 0); h0 < last - values; h0 += kAhead) {
                 float x[kAhead][8];
@@ -281,7 +340,8 @@ void append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int
     const int64_t tok_end = min(start + append_count(a, seq), static_cast<int64_t>(a.pt.stride) * kWave);
     const int64_t first_tile = start / kWave + static_cast<int64_t>(run) * tiles_per_group;
     if (max(first_tile * kWave, start) >= tok_end) return;
-    const int64_t head_base = seq * a.k_seq + kvh * a.k_head + col, pos0 = append_position(a, seq, start) - start;
+    const int64_t head_base = seq * a.k_seq + kvh * a.k_head + col;
+    const auto turns = turn.of(a, seq, start);
     const uint32_t sbits = a.signs[kvh * LPR + col / 8];
 
     // a tile's key rows: eight coordinates per thread and pass, rotated; rows outside [start, tok_end) are zeros
@@ -331,7 +391,7 @@ void append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int
             const int key = pass * RPP + tid / LPR;
             float (&x)[8] = rows[pass];
             RowRotation<LPR> rot;
-            rot.load(a.rope, pos0 + tile * kWave + key, col);
+            turns.load(rot, a, tile * kWave + key, col);
             rot.apply(x, lane);
             float ss = 0.0f;
 #pragma unroll
@@ -428,11 +488,25 @@ void append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int
     }
 }
 
+#define OCTOPUS_TILE_KERNEL                          \
+    __global__ __launch_bounds__(encode_threads<P>()) \
+    __attribute__((amdgpu_waves_per_eu(encode_waves_per_simd<P, false, true>(), encode_waves_per_simd<P, false, true>()))) void
 template <class P>
-int launch_append_plan(const octopus_codebooks_t &cb, const AppendCall &a, hipStream_t stream) {
-    const DeviceBooks books = device_books(cb);
+OCTOPUS_TILE_KERNEL append_tile_kernel(DeviceBooks books, AppendCall a, int32_t key_blocks, int32_t tile_runs, int32_t tiles_per_group, int32_t every) {
+    append_tile<P>(a, OneAxis{}, key_blocks, tile_runs, tiles_per_group, every);
+}
+template <class P>
+OCTOPUS_TILE_KERNEL append_tile_axes_kernel(DeviceBooks books, AppendCall a, ManyAxes turn, int32_t key_blocks, int32_t tile_runs, int32_t tiles_per_group,
+                                            int32_t every) {
+    append_tile<P>(a, turn, key_blocks, tile_runs, tiles_per_group, every);
+}
+#undef OCTOPUS_TILE_KERNEL
+
+// The launch of a call: token(grid, threads) for few tokens, else tile(grid, threads, key blocks, runs, tiles a run, every).
+template <class P, class Token, class Tile>
+int launch_append_shape(const AppendCall &a, Token token, Tile tile) {
     if (few_keys<P::D>(a.n_seq, a.n_kv_heads, a.n_new)) {
-        hipLaunchKernelGGL(append_token_kernel<P>, dim3(a.n_new, a.n_kv_heads, a.n_seq), dim3(kWave), 0, stream, books, a);
+        token(dim3(a.n_new, a.n_kv_heads, a.n_seq), dim3(kWave));
         return static_cast<int>(hipGetLastError());
     }
     constexpr int RPP = encode_threads<P>() / (P::D / 8);
@@ -443,9 +517,30 @@ int launch_append_plan(const octopus_codebooks_t &cb, const AppendCall &a, hipSt
     const int64_t row_blocks = static_cast<int64_t>((rows + kAppendRows - 1) / kAppendRows) * ((a.n_new + RPP - 1) / RPP) * a.n_seq;
     const int64_t blocks = key_blocks + row_blocks;
     if (blocks > (1 << 22)) return static_cast<int>(hipErrorInvalidValue);   // (threads of a launch; the host has checked it)
-    hipLaunchKernelGGL(append_tile_kernel<P>, dim3(static_cast<unsigned>(blocks)), dim3(encode_threads<P>()), 0, stream, books, a,
-                       static_cast<int32_t>(key_blocks), runs, per, static_cast<int32_t>(blocks / key_blocks));
+    tile(dim3(static_cast<unsigned>(blocks)), dim3(encode_threads<P>()), static_cast<int32_t>(key_blocks), runs, per,
+         static_cast<int32_t>(blocks / key_blocks));
     return static_cast<int>(hipGetLastError());
+}
+
+template <class P>
+int launch_append_plan(const octopus_codebooks_t &cb, const AppendCall &a, hipStream_t stream) {
+    const DeviceBooks books = device_books(cb);
+    return launch_append_shape<P>(
+        a, [&](dim3 grid, dim3 threads) { hipLaunchKernelGGL(append_token_kernel<P>, grid, threads, 0, stream, books, a); },
+        [&](dim3 grid, dim3 threads, int32_t key_blocks, int32_t runs, int32_t per, int32_t every) {
+            hipLaunchKernelGGL(append_tile_kernel<P>, grid, threads, 0, stream, books, a, key_blocks, runs, per, every);
+        });
+}
+
+template <class P>
+int launch_append_axes_plan(const octopus_codebooks_t &cb, const AppendCall &a, hipStream_t stream) {
+    const DeviceBooks books = device_books(cb);
+    const ManyAxes turn{*a.axes};
+    return launch_append_shape<P>(
+        a, [&](dim3 grid, dim3 threads) { hipLaunchKernelGGL(append_token_axes_kernel<P>, grid, threads, 0, stream, books, a, turn); },
+        [&](dim3 grid, dim3 threads, int32_t key_blocks, int32_t runs, int32_t per, int32_t every) {
+            hipLaunchKernelGGL(append_tile_axes_kernel<P>, grid, threads, 0, stream, books, a, turn, key_blocks, runs, per, every);
+        });
 }
 
 }  // namespace octopus

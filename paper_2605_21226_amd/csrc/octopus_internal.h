@@ -189,6 +189,15 @@ struct RopeCall {
     const int32_t *pos;
     int32_t dim, interleaved;
 };
+// ... by positions of several axes: axis k of token t of sequence s at pos[s stride_seq + t stride_tok + k stride_axis], pair i by axis
+// (axis_of[i / 16] >> 2 (i % 16)) & 3 (RopeCall::pos is not looked at).
+constexpr int kMaxAxes = OCTOPUS_MAX_AXES;
+struct AxesCall {
+    const int32_t *pos;
+    int64_t stride_seq, stride_tok, stride_axis;
+    uint32_t axis_of[8];
+    int32_t n_axes;
+};
 // Appending to pages (octopus_append.hpp).  v_pool NULL: the values are quantised by a launch of their own; q NULL: no queries.
 struct AppendCall {
     const void *k, *v, *q;
@@ -200,6 +209,7 @@ struct AppendCall {
     PageTable pt;
     int32_t n_seq, n_kv_heads, n_q_heads, n_new;
     int32_t kv_is_bf16, q_is_bf16, q_out_is_bf16;
+    const AxesCall *axes;   // host memory, or NULL: one position a token
 };
 int launch_append(const octopus_codebooks_t &cb, const AppendCall &a, void *stream);
 int launch_append_values(const AppendCall &a, int32_t head_dim, int32_t bits, int32_t group, void *vq_pool, void *stream);

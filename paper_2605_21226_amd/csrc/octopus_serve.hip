@@ -8,6 +8,7 @@ namespace octopus {
     int launch_prefix_d##D(const octopus_codebooks_t &, const PrefixShape &, const void *, const void *, const int32_t *, \
                            const int32_t *, const int32_t *, const int32_t *, const int32_t *, float *, float *, void *); \
     int launch_append_d##D(const octopus_codebooks_t &, const AppendCall &, void *);                                      \
+    int launch_append_axes_d##D(const octopus_codebooks_t &, const AppendCall &, void *);                                 \
     int launch_read_d##D(const octopus_codebooks_t &, const ReadCall &, void *);
 OCTOPUS_DECL(64)
 OCTOPUS_DECL(128)
@@ -30,6 +31,9 @@ int launch_prefix(const octopus_codebooks_t &cb, const PrefixShape &s, const voi
 }
 
 int launch_append(const octopus_codebooks_t &cb, const AppendCall &a, void *stream) {
+    if (a.axes != nullptr) {
+        OCTOPUS_BY_HEAD_DIM(cb.plan, launch_append_axes, cb, a, stream)
+    }
     OCTOPUS_BY_HEAD_DIM(cb.plan, launch_append, cb, a, stream)
 }
 

@@ -41,6 +41,92 @@ constexpr int64_t kMostRanges = 128;
 int64_t prefix_round_keys(const octopus_plan_t &plan) { return 32 * prefix_waves(plan.head_dim); }
 int64_t most_ranges(int64_t rows) { return std::min(std::max<int64_t>(kRangePartials / rows, 1), kMostRanges); }
 
+// octopus_append_paged (axes NULL) and octopus_append_paged_axes (rope NULL).
+int append(const octopus_codebooks_t *cb, const void *k, int64_t k_stride_seq, int64_t k_stride_tok, int64_t k_stride_head,
+           const void *v, int64_t v_stride_seq, int64_t v_stride_tok, int64_t v_stride_head, int32_t kv_dtype, int32_t n_seq,
+           int32_t n_kv_heads, int32_t n_new, const int32_t *new_lens, const octopus_rope_t *rope, const octopus_rope_axes_t *axes, const void *q,
+           int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head, int32_t n_q_heads, void *q_out,
+           int32_t q_out_dtype, const uint8_t *signs, void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group,
+           int32_t n_pages, const int32_t *block_table, int32_t max_pages_per_seq, const int32_t *start_pos, void *stream) {
+    if (cb == nullptr || signs == nullptr || k_pool == nullptr || v_pool == nullptr) return OCTOPUS_EINVAL;
+    if (n_new != 0 && (k == nullptr || v == nullptr)) return OCTOPUS_EINVAL;   // (an empty tensor may have no address)
+    if (n_seq < 1 || n_kv_heads < 1 || n_new < 0 || n_seq > 65535 || n_kv_heads > 65535 || n_pages < 1) return OCTOPUS_EINVAL;
+    if (!pages_ok(block_table, max_pages_per_seq) || !plan_well_formed(cb->plan)) return OCTOPUS_EINVAL;
+    const int32_t d = cb->plan.head_dim;
+    auto type_ok = [](int32_t t) { return t == OCTOPUS_DTYPE_F32 || t == OCTOPUS_DTYPE_BF16; };
+    if (!type_ok(kv_dtype) || !plan_supported(cb->plan) || !encoder_takes(*cb) || !corner_levels(*cb)) return OCTOPUS_EUNSUPPORTED;
+    if (v_bits != 0 && (v_bits < 2 || v_bits > 4 || (v_group != 16 && v_group != 32))) return OCTOPUS_EUNSUPPORTED;
+    auto strides_ok = [](int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && a % 8 == 0 && b % 8 == 0 && c % 8 == 0; };
+    if (!strides_ok(k_stride_seq, k_stride_tok, k_stride_head) || !strides_ok(v_stride_seq, v_stride_tok, v_stride_head)) return OCTOPUS_EINVAL;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(new_lens, 4) || !aligned(start_pos, 4))
+        return OCTOPUS_EINVAL;
+    AppendCall a{};
+    if (q != nullptr) {
+        if (q_out == nullptr || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) return OCTOPUS_EINVAL;
+        if (!type_ok(q_dtype) || !type_ok(q_out_dtype)) return OCTOPUS_EUNSUPPORTED;
+        if (!strides_ok(q_stride_seq, q_stride_tok, q_stride_head) || !aligned(q, 16) || !aligned(q_out, 16)) return OCTOPUS_EINVAL;
+        a.n_q_heads = n_q_heads;
+    }
+    if (rope != nullptr) {
+        if (rope->table == nullptr || !aligned(rope->table, 16) || rope->n_pos < 1 || !aligned(rope->pos, 4)) return OCTOPUS_EINVAL;
+        if (rope->dim < 16 || rope->dim > d || rope->dim % 16 != 0 || (rope->interleaved != 0 && rope->interleaved != 1)) return OCTOPUS_EINVAL;
+        a.rope = RopeCall{rope->table, rope->n_pos, rope->pos, rope->dim, rope->interleaved};
+    }
+    AxesCall many{};
+    if (axes != nullptr) {
+        if (axes->table == nullptr || !aligned(axes->table, 16) || axes->n_pos < 1 || axes->pos == nullptr || !aligned(axes->pos, 4)) return OCTOPUS_EINVAL;
+        if (axes->dim < 16 || axes->dim > d || axes->dim % 16 != 0 || (axes->interleaved != 0 && axes->interleaved != 1)) return OCTOPUS_EINVAL;
+        if (axes->stride_seq < 0 || axes->stride_tok < 0 || axes->stride_axis < 0) return OCTOPUS_EINVAL;
+        if (axes->n_axes < 1 || axes->n_axes > kMaxAxes || axes->axis == nullptr) return OCTOPUS_EINVAL;
+        for (int i = 0; i < axes->dim / 2; ++i) {
+            if (axes->axis[i] >= axes->n_axes) return OCTOPUS_EINVAL;
+            many.axis_of[i / 16] |= static_cast<uint32_t>(axes->axis[i]) << (2 * (i % 16));
+        }
+        many.pos = axes->pos;
+        many.stride_seq = axes->stride_seq;
+        many.stride_tok = axes->stride_tok;
+        many.stride_axis = axes->stride_axis;
+        many.n_axes = axes->n_axes;
+        a.rope = RopeCall{axes->table, axes->n_pos, nullptr, axes->dim, axes->interleaved};
+        a.axes = &many;
+    }
+    if (start_pos == nullptr && n_new > static_cast<int64_t>(max_pages_per_seq) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
+    // the launch: 2^22 workgroups at most, of tiles and of runs of at least 16 tokens by eight rows
+    const int64_t tiles = (static_cast<int64_t>(n_new) / 64 + 2) * n_kv_heads * n_seq;
+    const int64_t rows = (static_cast<int64_t>(n_kv_heads) + a.n_q_heads) / 8 + 1, runs = (static_cast<int64_t>(n_new) / 16 + 1) * n_seq;
+    if (tiles > (1 << 21) || rows > (1 << 21) || rows * runs > (1 << 21)) return OCTOPUS_EINVAL;
+    if (v_bits != 0 && static_cast<int64_t>(n_kv_heads) * (d / v_group) > 4096) return OCTOPUS_EINVAL;
+    if (n_new == 0) return OCTOPUS_OK;
+    a.k = k;
+    a.v = v;
+    a.q = q;
+    a.k_seq = k_stride_seq;
+    a.k_tok = k_stride_tok;
+    a.k_head = k_stride_head;
+    a.v_seq = v_stride_seq;
+    a.v_tok = v_stride_tok;
+    a.v_head = v_stride_head;
+    a.q_seq = q_stride_seq;
+    a.q_tok = q_stride_tok;
+    a.q_head = q_stride_head;
+    a.k_pool = k_pool;
+    a.v_pool = v_bits == 0 ? v_pool : nullptr;
+    a.q_out = q_out;
+    a.signs = signs;
+    a.start_pos = start_pos;
+    a.new_lens = new_lens;
+    a.pt = PageTable{block_table, max_pages_per_seq, n_pages};
+    a.n_seq = n_seq;
+    a.n_kv_heads = n_kv_heads;
+    a.n_new = n_new;
+    a.kv_is_bf16 = kv_dtype == OCTOPUS_DTYPE_BF16;
+    a.q_is_bf16 = q_dtype == OCTOPUS_DTYPE_BF16;
+    a.q_out_is_bf16 = q_out_dtype == OCTOPUS_DTYPE_BF16;
+    int err = launch_append(*cb, a, stream);
+    if (err == 0 && v_bits != 0) err = launch_append_values(a, d, v_bits, v_group, v_pool, stream);
+    return err == 0 ? OCTOPUS_OK : OCTOPUS_EHIP;
+}
+
 }  // namespace
 
 int64_t prefix_room(const octopus_plan_t &plan, int64_t rows, int64_t max_prefix, int64_t max_len) {
@@ -162,65 +248,21 @@ int octopus_append_paged(const octopus_codebooks_t *cb, const void *k, int64_t k
                          int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head, int32_t n_q_heads, void *q_out,
                          int32_t q_out_dtype, const uint8_t *signs, void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group,
                          int32_t n_pages, const int32_t *block_table, int32_t max_pages_per_seq, const int32_t *start_pos, void *stream) {
-    if (cb == nullptr || signs == nullptr || k_pool == nullptr || v_pool == nullptr) return OCTOPUS_EINVAL;
-    if (n_new != 0 && (k == nullptr || v == nullptr)) return OCTOPUS_EINVAL;   // (an empty tensor may have no address)
-    if (n_seq < 1 || n_kv_heads < 1 || n_new < 0 || n_seq > 65535 || n_kv_heads > 65535 || n_pages < 1) return OCTOPUS_EINVAL;
-    if (!pages_ok(block_table, max_pages_per_seq) || !plan_well_formed(cb->plan)) return OCTOPUS_EINVAL;
-    const int32_t d = cb->plan.head_dim;
-    auto type_ok = [](int32_t t) { return t == OCTOPUS_DTYPE_F32 || t == OCTOPUS_DTYPE_BF16; };
-    if (!type_ok(kv_dtype) || !plan_supported(cb->plan) || !encoder_takes(*cb) || !corner_levels(*cb)) return OCTOPUS_EUNSUPPORTED;
-    if (v_bits != 0 && (v_bits < 2 || v_bits > 4 || (v_group != 16 && v_group != 32))) return OCTOPUS_EUNSUPPORTED;
-    auto strides_ok = [](int64_t a, int64_t b, int64_t c) { return a >= 0 && b >= 0 && c >= 0 && a % 8 == 0 && b % 8 == 0 && c % 8 == 0; };
-    if (!strides_ok(k_stride_seq, k_stride_tok, k_stride_head) || !strides_ok(v_stride_seq, v_stride_tok, v_stride_head)) return OCTOPUS_EINVAL;
-    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(new_lens, 4) || !aligned(start_pos, 4))
-        return OCTOPUS_EINVAL;
-    AppendCall a{};
-    if (q != nullptr) {
-        if (q_out == nullptr || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) return OCTOPUS_EINVAL;
-        if (!type_ok(q_dtype) || !type_ok(q_out_dtype)) return OCTOPUS_EUNSUPPORTED;
-        if (!strides_ok(q_stride_seq, q_stride_tok, q_stride_head) || !aligned(q, 16) || !aligned(q_out, 16)) return OCTOPUS_EINVAL;
-        a.n_q_heads = n_q_heads;
-    }
-    if (rope != nullptr) {
-        if (rope->table == nullptr || !aligned(rope->table, 16) || rope->n_pos < 1 || !aligned(rope->pos, 4)) return OCTOPUS_EINVAL;
-        if (rope->dim < 16 || rope->dim > d || rope->dim % 16 != 0 || (rope->interleaved != 0 && rope->interleaved != 1)) return OCTOPUS_EINVAL;
-        a.rope = RopeCall{rope->table, rope->n_pos, rope->pos, rope->dim, rope->interleaved};
-    }
-    if (start_pos == nullptr && n_new > static_cast<int64_t>(max_pages_per_seq) * OCTOPUS_TILE) return OCTOPUS_EINVAL;
-    // the launch: 2^22 workgroups at most, of tiles and of runs of at least 16 tokens by eight rows
-    const int64_t tiles = (static_cast<int64_t>(n_new) / 64 + 2) * n_kv_heads * n_seq;
-    const int64_t rows = (static_cast<int64_t>(n_kv_heads) + a.n_q_heads) / 8 + 1, runs = (static_cast<int64_t>(n_new) / 16 + 1) * n_seq;
-    if (tiles > (1 << 21) || rows > (1 << 21) || rows * runs > (1 << 21)) return OCTOPUS_EINVAL;
-    if (v_bits != 0 && static_cast<int64_t>(n_kv_heads) * (d / v_group) > 4096) return OCTOPUS_EINVAL;
-    if (n_new == 0) return OCTOPUS_OK;
-    a.k = k;
-    a.v = v;
-    a.q = q;
-    a.k_seq = k_stride_seq;
-    a.k_tok = k_stride_tok;
-    a.k_head = k_stride_head;
-    a.v_seq = v_stride_seq;
-    a.v_tok = v_stride_tok;
-    a.v_head = v_stride_head;
-    a.q_seq = q_stride_seq;
-    a.q_tok = q_stride_tok;
-    a.q_head = q_stride_head;
-    a.k_pool = k_pool;
-    a.v_pool = v_bits == 0 ? v_pool : nullptr;
-    a.q_out = q_out;
-    a.signs = signs;
-    a.start_pos = start_pos;
-    a.new_lens = new_lens;
-    a.pt = PageTable{block_table, max_pages_per_seq, n_pages};
-    a.n_seq = n_seq;
-    a.n_kv_heads = n_kv_heads;
-    a.n_new = n_new;
-    a.kv_is_bf16 = kv_dtype == OCTOPUS_DTYPE_BF16;
-    a.q_is_bf16 = q_dtype == OCTOPUS_DTYPE_BF16;
-    a.q_out_is_bf16 = q_out_dtype == OCTOPUS_DTYPE_BF16;
-    int err = launch_append(*cb, a, stream);
-    if (err == 0 && v_bits != 0) err = launch_append_values(a, d, v_bits, v_group, v_pool, stream);
-    return err == 0 ? OCTOPUS_OK : OCTOPUS_EHIP;
+    return append(cb, k, k_stride_seq, k_stride_tok, k_stride_head, v, v_stride_seq, v_stride_tok, v_stride_head, kv_dtype, n_seq,
+                  n_kv_heads, n_new, new_lens, rope, nullptr, q, q_dtype, q_stride_seq, q_stride_tok, q_stride_head, n_q_heads, q_out,
+                  q_out_dtype, signs, k_pool, v_pool, v_bits, v_group, n_pages, block_table, max_pages_per_seq, start_pos, stream);
+}
+
+int octopus_append_paged_axes(const octopus_codebooks_t *cb, const void *k, int64_t k_stride_seq, int64_t k_stride_tok, int64_t k_stride_head,
+                              const void *v, int64_t v_stride_seq, int64_t v_stride_tok, int64_t v_stride_head, int32_t kv_dtype, int32_t n_seq,
+                              int32_t n_kv_heads, int32_t n_new, const int32_t *new_lens, const octopus_rope_axes_t *rope, const void *q,
+                              int32_t q_dtype, int64_t q_stride_seq, int64_t q_stride_tok, int64_t q_stride_head, int32_t n_q_heads, void *q_out,
+                              int32_t q_out_dtype, const uint8_t *signs, void *k_pool, void *v_pool, int32_t v_bits, int32_t v_group,
+                              int32_t n_pages, const int32_t *block_table, int32_t max_pages_per_seq, const int32_t *start_pos, void *stream) {
+    if (rope == nullptr) return OCTOPUS_EINVAL;
+    return append(cb, k, k_stride_seq, k_stride_tok, k_stride_head, v, v_stride_seq, v_stride_tok, v_stride_head, kv_dtype, n_seq,
+                  n_kv_heads, n_new, new_lens, nullptr, rope, q, q_dtype, q_stride_seq, q_stride_tok, q_stride_head, n_q_heads, q_out,
+                  q_out_dtype, signs, k_pool, v_pool, v_bits, v_group, n_pages, block_table, max_pages_per_seq, start_pos, stream);
 }
 
 int octopus_read_paged(const octopus_codebooks_t *cb, const uint8_t *signs, const void *k_pool, const void *v_pool, int32_t v_bits,
