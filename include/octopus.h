@@ -19,6 +19,8 @@
  *                                                  a step's keys, values and queries, rotated by position (on one axis or
  *                                                  several), into pages; tokens of pages as values again
  *   octopus_attn_decode_paged_prefix               attention of sequences that share a prefix
+ *   octopus_pages_update, octopus_pages_copy, octopus_pages_compact, octopus_pages_rename
+ *                                                  who holds which page: forks, growth, trimming, freeing, compaction
  *
  * Conventions
  *   - Plain C.  Every function returns 0 (OCTOPUS_OK) or a negative error
@@ -642,6 +644,79 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb,
                                      float *out,
                                      void *workspace, size_t workspace_bytes,
                                      void *stream);
+
+/* ---- the pages themselves: who holds which (forks, growth, trimming, freeing), compaction, copying ----
+ * A server's page bookkeeping in device memory, changed on the caller's stream without a host read, so that the steps around it (appending,
+ * attention, verifying drafts) can be captured with it.  The state is
+ *   refs         device int32 [n_pages], 16-byte aligned: how many table entries hold the page; 0 or less: it is free.  A page that something
+ *                else holds (a prefix_table, a cache of prompts) is counted there by the caller: 1 more for each.
+ *   block_table, max_pages_per_seq, lens   a table as for octopus_encode_paged and, device int32 [n_seq], the tokens of each slot: slot s
+ *                holds the pages of entries below ceil(lens[s] / 64), once each; the other entries mean nothing and are left as they are.
+ * It serves all pools that go by the table: keys, values, side-cars, of every layer.
+ *
+ * octopus_pages_update: every slot s becomes a continuation of slot source[s] (NULL: of itself): it holds the pages of the first
+ *       kept = min(lens[source[s]], keep_lens[s], new_lens[s])
+ *   tokens of that slot's old row (keep_lens NULL: as many as there are), and pages for new_lens[s] tokens in all; lens[s] = new_lens[s].  That is
+ *   a step's growth (new_lens above lens), a trim to the accepted drafts (keep_lens) with the growth for the next ones, a fork
+ *   (two slots of one source: beams, samples), a slot that moves, and one that ends (new_lens 0, or a source outside [0, n_seq), of which nothing
+ *   is kept).  Slots' pages are counted, and free when nobody holds them any longer.  Where the kept tokens end inside a page and the slot
+ *   grows, that page will be written into, so it has to be the slot's own: of several slots that would write into the same page the first
+ *   keeps it if nobody else holds it (one whose source is itself before the others), and each of the others holds a free page in its
+ *   place and is listed in `moves`.
+ *   Free pages are handed out lowest number first, to the slots in order; a slot's copied page comes first.
+ *   If there are fewer than are needed, no slot grows: every lens[s] is the tokens kept, no page is to be copied, and moves[1] says how
+ *   many are missing.
+ *     source, keep_lens, new_lens   device int32 [n_seq] (the first two may be NULL); token counts are clamped to what a row holds, page ids to the pool.
+ *     moves      device int32 [2 + 2 n_seq]: [0] pages to be copied, [1] pages missing, then (from, to) pairs in the order of slots.  Give it
+ *                to octopus_pages_copy before anything is appended; no page is both a from and a to.
+ *     workspace  device, 256-byte aligned, octopus_pages_workspace(...) bytes of the same shape (which does not shrink as a number grows);
+ *                contents are scratch.
+ *   One launch; three with a source.
+ *
+ * octopus_pages_compact: moves the pages in use to the front of the pools: with n of them in use, the highest goes to the lowest free one, the next
+ *   to the next, until they are 0 .. n - 1.
+ *     page_map   device int32 [n_pages]: a page's new number (its own where it stays).
+ *     moves      device int32 [2 + 2 (n_pages / 2)]: [0] pages to be copied, [1] n, then (from, to) pairs, highest page first.
+ *   refs follow.  Every table has to follow by octopus_pages_rename, and every pool by octopus_pages_copy.  Three launches.
+ * octopus_pages_rename: entries below ceil(lens[r] / 64) of each row r (lens NULL: all) become page_map[entry]; a block table, or
+ *   (n_rows 1, prefix_len) a prefix_table.
+ *
+ * octopus_pages_copy: page moves[2 + 2 i] of every pool to page moves[3 + 2 i], i < moves[0].
+ *     pools      host array, read before the call returns: data device, 16-byte aligned, n_pages pages of page_bytes bytes, a multiple of 16
+ *                (octopus_paged_pool_bytes(cb, 1, n_kv_heads), 128 n_kv_heads head_dim, octopus_vq_bytes(head_dim, bits, group, 1,
+ *                n_kv_heads, 64), octopus_qjl_bytes(cb, 1, n_kv_heads, 64)); no two of them overlap.
+ *     moves      device, as above, or the caller's own: its second number is not looked at.  Pairs with a number outside [0, n_pages) are
+ *                left out; a page may be the `to` of one pair only and not the `from` of another.
+ *     max_moves  host: pairs that `moves` has room for; moves[0] is clamped to it.
+ *   One launch for every 64 pools.
+ * Errors: EINVAL (NULL or misaligned pointers; n_pages outside 1 .. 2^24, n_seq or n_rows outside 1 .. 65535, more than 2^30 table entries,
+ * no pools, a negative max_moves, page_bytes that are no positive multiple of 16 or over 2^40 bytes in all), EWORKSPACE, EHIP. */
+typedef struct octopus_pool {
+    void *data;
+    int64_t page_bytes;
+} octopus_pool_t;
+
+size_t octopus_pages_workspace(int32_t n_pages, int32_t n_seq, int32_t max_pages_per_seq);
+
+int octopus_pages_update(int32_t *refs, int32_t n_pages,
+                         int32_t *block_table, int32_t max_pages_per_seq, int32_t *lens, int32_t n_seq,
+                         const int32_t *source, const int32_t *keep_lens, const int32_t *new_lens,
+                         int32_t *moves,
+                         void *workspace, size_t workspace_bytes,
+                         void *stream);
+
+int octopus_pages_compact(int32_t *refs, int32_t n_pages,
+                          int32_t *page_map, int32_t *moves,
+                          void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+int octopus_pages_rename(const int32_t *page_map, int32_t n_pages,
+                         int32_t *table, int32_t n_rows, int32_t max_pages_per_row, const int32_t *lens,
+                         void *stream);
+
+int octopus_pages_copy(const octopus_pool_t *pools, int32_t n_pools, int32_t n_pages,
+                       const int32_t *moves, int32_t max_moves,
+                       void *stream);
 
 /* Static, human-readable name of an error code. */
 const char *octopus_strerror(int code);

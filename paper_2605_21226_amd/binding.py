@@ -28,7 +28,8 @@ EXPORTS = ("octopus_build_codebooks", "octopus_build_codebooks_pair", "octopus_c
            "octopus_encode_qjl_paged", "octopus_attn_decode_paged_qjl",
            "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores",
            "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix",
-           "octopus_append_paged", "octopus_append_paged_axes", "octopus_read_paged")
+           "octopus_append_paged", "octopus_append_paged_axes", "octopus_read_paged",
+           "octopus_pages_workspace", "octopus_pages_update", "octopus_pages_copy", "octopus_pages_compact", "octopus_pages_rename")
 
 
 class Plan(ctypes.Structure):
@@ -78,6 +79,13 @@ class RopeAxes(ctypes.Structure):
         ("n_axes", ctypes.c_int32),
         ("dim", ctypes.c_int32),
         ("interleaved", ctypes.c_int32),
+    ]
+
+
+class Pool(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("page_bytes", ctypes.c_int64),
     ]
 
 
@@ -174,6 +182,16 @@ def load():
     lib.octopus_append_paged_axes.restype = ctypes.c_int
     lib.octopus_read_paged.argtypes = [CB, vp, vp, vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, vp, vp, vp, i32, vp]
     lib.octopus_read_paged.restype = ctypes.c_int
+    lib.octopus_pages_workspace.argtypes = [i32, i32, i32]
+    lib.octopus_pages_workspace.restype = ctypes.c_size_t
+    lib.octopus_pages_update.argtypes = [vp, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.octopus_pages_update.restype = ctypes.c_int
+    lib.octopus_pages_compact.argtypes = [vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.octopus_pages_compact.restype = ctypes.c_int
+    lib.octopus_pages_rename.argtypes = [vp, i32, vp, i32, i32, vp, vp]
+    lib.octopus_pages_rename.restype = ctypes.c_int
+    lib.octopus_pages_copy.argtypes = [ctypes.POINTER(Pool), i32, i32, vp, i32, vp]
+    lib.octopus_pages_copy.restype = ctypes.c_int
     lib.octopus_vq_on_matrix_cores.argtypes = [ctypes.POINTER(Codebooks), i32, i32, i32, i32, i32]
     lib.octopus_vq_on_matrix_cores.restype = ctypes.c_int
     lib.octopus_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
@@ -625,6 +643,71 @@ def octopus_read_paged(cb, signs, k_pool, v_pool, n_pages, block_table, k_out, v
         max_pages, n_seq, n_kv, _ptr(start_pos), n_tok, _ptr(lens), _ptr(k_out), _ptr(v_out), _dtype_code(like),
         _stream_ptr(stream))
     _check(code, "octopus_read_paged")
+
+
+def octopus_pages_workspace(n_pages, n_seq, max_pages_per_seq):
+    return int(load().octopus_pages_workspace(int(n_pages), int(n_seq), int(max_pages_per_seq)))
+
+
+def _check_ints(*tensors):
+    """That each (tensor or None, least number of elements) is contiguous int32 of at least as many."""
+    for t, least in tensors:
+        assert t is None or (_is_int32(t) and t.is_contiguous() and t.numel() >= least)
+
+
+def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, source=None, keep_lens=None, stream=None):
+    """Slots continue themselves or source[s], keep min(lens, keep_lens, new_lens) tokens and get pages for new_lens: refs device int32
+    [n_pages], block_table device int32 [n_seq, max_pages_per_seq], lens, new_lens, source and keep_lens device int32 [n_seq], moves
+    device int32 of at least 2 + 2 n_seq, workspace device uint8 of octopus_pages_workspace(...)."""
+    n_seq, max_pages = block_table.shape
+    _check_ints((refs, 1), (block_table, 1), (lens, n_seq), (new_lens, n_seq), (source, n_seq), (keep_lens, n_seq), (moves, 2 + 2 * n_seq))
+    code = load().octopus_pages_update(refs.data_ptr(), refs.numel(), block_table.data_ptr(), max_pages, lens.data_ptr(), n_seq, _ptr(source),
+                                       _ptr(keep_lens), new_lens.data_ptr(), moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                                       _stream_ptr(stream))
+    _check(code, "octopus_pages_update")
+
+
+def octopus_pages_compact(refs, page_map, moves, workspace, stream=None):
+    """The pages in use to the front: refs and page_map device int32 [n_pages], moves device int32 of at least 2 + 2 (n_pages // 2)."""
+    n_pages = refs.numel()
+    _check_ints((refs, 1), (page_map, n_pages), (moves, 2 + 2 * (n_pages // 2)))
+    code = load().octopus_pages_compact(refs.data_ptr(), n_pages, page_map.data_ptr(), moves.data_ptr(), workspace.data_ptr(),
+                                        workspace.nbytes, _stream_ptr(stream))
+    _check(code, "octopus_pages_compact")
+
+
+def octopus_pages_rename(page_map, table, lens=None, stream=None):
+    """Entries of table (device int32 [n_rows, max_pages], or one row) below ceil(lens / 64) (lens device int32 [n_rows]; None: all) by page_map."""
+    n_rows, max_pages = table.shape if table.dim() == 2 else (1, table.numel())
+    _check_ints((page_map, 1), (table, 1), (lens, n_rows))
+    code = load().octopus_pages_rename(page_map.data_ptr(), page_map.numel(), table.data_ptr(), n_rows, max_pages, _ptr(lens),
+                                       _stream_ptr(stream))
+    _check(code, "octopus_pages_rename")
+
+
+class PagePools:
+    """The pools that octopus_pages_copy copies pages of; made once, by page_pools, and kept with the pools."""
+
+    def __init__(self, tensors, n_pages):
+        self.tensors, self.n_pages = tensors, n_pages
+        self.array = (Pool * len(tensors))(*[Pool(t.data_ptr(), t.nbytes // n_pages) for t in tensors])
+
+
+def page_pools(tensors, n_pages=None):
+    """tensors: device, contiguous, each n_pages pages (None: the first dimension of each)."""
+    tensors = list(tensors)
+    n_pages = tensors[0].shape[0] if n_pages is None else int(n_pages)
+    assert n_pages >= 1 and all(t.is_contiguous() and t.nbytes % n_pages == 0 for t in tensors)
+    assert all(t.dim() == 1 or t.shape[0] == n_pages for t in tensors)
+    return PagePools(tensors, n_pages)
+
+
+def octopus_pages_copy(pools, moves, max_moves=None, stream=None):
+    """Pages of every pool of `pools` (page_pools) by the (from, to) pairs of moves, device int32 [2 + 2 max_moves], of which moves[0] count."""
+    most = moves.numel() // 2 - 1 if max_moves is None else int(max_moves)
+    _check_ints((moves, 2 + 2 * max(most, 0)))
+    code = load().octopus_pages_copy(pools.array, len(pools.array), pools.n_pages, moves.data_ptr(), most, _stream_ptr(stream))
+    _check(code, "octopus_pages_copy")
 
 
 def octopus_profile_events(before, after):

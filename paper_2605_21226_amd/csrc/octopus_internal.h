@@ -227,6 +227,40 @@ struct ReadCall {
 };
 int launch_read(const octopus_codebooks_t &cb, const ReadCall &a, void *stream);
 
+// Who holds which page (octopus_pages.hip); the regions from `writers` on are scratch.
+struct alignas(16) SlotPages {
+    int32_t kept, want;     // tokens that the slot keeps of its source, tokens that it is to have
+    int32_t src;            // the source, -1: none
+    int32_t copied;         // 1: the page in which the kept tokens end is copied
+};
+struct PagesCall {
+    int32_t *refs;                      // [n_pages]: table entries that hold the page
+    int32_t *table, *lens;              // [n_seq][max_pages], [n_seq]
+    const int32_t *source, *keep_lens, *new_lens;   // [n_seq]; the first two may be NULL
+    int32_t *moves;                     // count, a second number, (from, to) pairs
+    int32_t *page_map;                  // [n_pages]
+    int32_t n_pages, max_pages, n_seq;
+    int32_t *writers, *first;           // [n_pages]: slots that write into a page, the first of them; compaction: pages in use of every 4096
+    int32_t *fresh;                     // [n_pages]: the free pages that are handed out
+    SlotPages *info;                    // [n_seq]
+    int32_t *staged;                    // [n_seq][max_pages]: rows that come from other slots
+};
+int launch_pages_update(const PagesCall &c, void *stream);
+int launch_pages_compact(const PagesCall &c, void *stream);
+int launch_pages_rename(const PagesCall &c, void *stream);
+// Copies pages moves[2 + 2 i] to moves[3 + 2 i] of up to kCopyPools pools.
+constexpr int32_t kCopyPools = 64;      // of a launch: their places are its arguments
+struct CopyPool {
+    void *data;
+    int64_t page_bytes;
+};
+struct CopyCall {
+    CopyPool pools[kCopyPools];
+    const int32_t *moves;
+    int32_t max_moves, n_pages;
+};
+int launch_pages_copy(const CopyCall &c, int32_t n_pools, void *stream);
+
 // What the entry points outside octopus_host.cpp ask of it: a plan whose parts fit together, codebooks the encoder takes, and the
 // measurement events armed for this thread's next decode-attention call (forgotten by the asking).
 bool plan_well_formed(const octopus_plan_t &plan);
