@@ -21,6 +21,7 @@
  *   octopus_attn_decode_paged_prefix               attention of sequences that share a prefix
  *   octopus_pages_update, octopus_pages_copy, octopus_pages_compact, octopus_pages_rename
  *                                                  who holds which page: forks, growth, trimming, freeing, compaction
+ *   octopus_verify_drafts                          drafted tokens against the target's probabilities
  *
  * Conventions
  *   - Plain C.  Every function returns 0 (OCTOPUS_OK) or a negative error
@@ -717,6 +718,40 @@ int octopus_pages_rename(const int32_t *page_map, int32_t n_pages,
 int octopus_pages_copy(const octopus_pool_t *pools, int32_t n_pools, int32_t n_pages,
                        const int32_t *moves, int32_t max_moves,
                        void *stream);
+
+/* ---- verification of drafted tokens against the target's probabilities, from given random numbers ----
+ * Sequence s has n = draft_lens[s] drafted tokens x_0 .. x_(n-1), x_i drawn from q_i, and the target's distributions p_0 .. p_n of the token after i
+ * of them (octopus_attn_decode_paged_prefix with causal takes a model there in one pass).  Draft i stands if u_i q_i(x_i) < p_i(x_i);
+ * a = the drafts before the first that does not stand (n: all stand).  The token after them is drawn from the weights
+ *       r(v) = max(p_a(v) - q_a(v), 0)  if a < n,    r(v) = p_n(v)  if a = n:
+ * it is the first token whose r is positive and whose running sum exceeds u' sum_v r(v), u' being the sequence's last random number.  So drafts
+ * and token are distributed as the target's own tokens would be.  Differences and sums are 64-bit numbers.
+ *   target       device, p_i(v) of sequence s at s*target_stride_seq + i*target_stride_pos + v, v in [0, vocab); i <= n_draft; dtype F32/BF16
+ *                (of both).  Rows need not sum to one: each is taken as it is for the test of its draft, and its sum for the draw.
+ *   draft        device, q_i(v) like target (i < n_draft), or NULL: drafts that were not drawn (looked up in the prompt, the drafter's likeliest): q_i is
+ *                1 at x_i, 0 elsewhere.
+ *   draft_tokens device int32 [n_seq][n_draft]; one outside [0, vocab) does not stand, nor does any where p_i(x_i) is 0.
+ *   draft_lens   device int32 [n_seq] or NULL (all n_draft), clamped to 0 .. n_draft; rows behind p_n are not looked at.
+ *   uniforms     device fp32 [n_seq][n_draft + 1], in [0, 1) (one outside is read as the nearest inside, NaN as 0): the drafts', and the last one for the
+ *                token.
+ *   tokens_out   device int32 [n_seq][n_draft + 1]: the drafts that stand, the token, then -1.
+ *   n_accepted   device int32 [n_seq]: a.  (Of a + 1 tokens the cache holds the first a once trimmed: octopus_pages_update.)
+ *   workspace    device, 256-byte aligned, at least octopus_verify_workspace(...) bytes (which does not shrink as a number grows); scratch.
+ * Probabilities that are no positive finite numbers count as 0.  Where no r(v) is positive though a draft fell, the token is drawn from p_a;
+ * where no p_a(v) is either, it is -1.  n_draft 0 (draft and draft_tokens NULL): one token drawn from each sequence's p_0.
+ * Two launches.  Outputs overlap no input.
+ * Errors: EINVAL (NULL or misaligned pointers, negative strides, n_seq outside 1 .. 65535, n_draft outside 0 .. 2^20, vocab outside 1 .. 2^30),
+ * EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */
+size_t octopus_verify_workspace(int32_t n_seq, int32_t n_draft, int32_t vocab);
+
+int octopus_verify_drafts(const void *target, int32_t dtype, int64_t target_stride_seq, int64_t target_stride_pos,
+                          const void *draft, int64_t draft_stride_seq, int64_t draft_stride_pos,
+                          const int32_t *draft_tokens, const int32_t *draft_lens,
+                          const float *uniforms,
+                          int32_t n_seq, int32_t n_draft, int32_t vocab,
+                          int32_t *tokens_out, int32_t *n_accepted,
+                          void *workspace, size_t workspace_bytes,
+                          void *stream);
 
 /* Static, human-readable name of an error code. */
 const char *octopus_strerror(int code);

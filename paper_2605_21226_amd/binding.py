@@ -29,7 +29,8 @@ EXPORTS = ("octopus_build_codebooks", "octopus_build_codebooks_pair", "octopus_c
            "octopus_attn_decode_static", "octopus_probe_read", "octopus_vq_on_matrix_cores",
            "octopus_attn_prefix_workspace", "octopus_attn_decode_paged_prefix",
            "octopus_append_paged", "octopus_append_paged_axes", "octopus_read_paged",
-           "octopus_pages_workspace", "octopus_pages_update", "octopus_pages_copy", "octopus_pages_compact", "octopus_pages_rename")
+           "octopus_pages_workspace", "octopus_pages_update", "octopus_pages_copy", "octopus_pages_compact", "octopus_pages_rename",
+           "octopus_verify_workspace", "octopus_verify_drafts")
 
 
 class Plan(ctypes.Structure):
@@ -192,6 +193,10 @@ def load():
     lib.octopus_pages_rename.restype = ctypes.c_int
     lib.octopus_pages_copy.argtypes = [ctypes.POINTER(Pool), i32, i32, vp, i32, vp]
     lib.octopus_pages_copy.restype = ctypes.c_int
+    lib.octopus_verify_workspace.argtypes = [i32, i32, i32]
+    lib.octopus_verify_workspace.restype = ctypes.c_size_t
+    lib.octopus_verify_drafts.argtypes = [vp, i32, i64, i64, vp, i64, i64, vp, vp, vp, i32, i32, i32, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.octopus_verify_drafts.restype = ctypes.c_int
     lib.octopus_vq_on_matrix_cores.argtypes = [ctypes.POINTER(Codebooks), i32, i32, i32, i32, i32]
     lib.octopus_vq_on_matrix_cores.restype = ctypes.c_int
     lib.octopus_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
@@ -708,6 +713,32 @@ def octopus_pages_copy(pools, moves, max_moves=None, stream=None):
     _check_ints((moves, 2 + 2 * max(most, 0)))
     code = load().octopus_pages_copy(pools.array, len(pools.array), pools.n_pages, moves.data_ptr(), most, _stream_ptr(stream))
     _check(code, "octopus_pages_copy")
+
+
+def octopus_verify_workspace(n_seq, n_draft, vocab):
+    return int(load().octopus_verify_workspace(int(n_seq), int(n_draft), int(vocab)))
+
+
+def octopus_verify_drafts(target, draft, draft_tokens, uniforms, tokens_out, n_accepted, workspace, draft_lens=None, stream=None):
+    """Drafted tokens against the target's probabilities: target device [n_seq, n_draft + 1, vocab] and draft [n_seq, n_draft, vocab] of one type
+    (any strides with a contiguous last dimension; draft None: drafts that were not drawn), draft_tokens device int32 [n_seq, n_draft] (None
+    with no drafts), uniforms device fp32 [n_seq, n_draft + 1], tokens_out device int32 [n_seq, n_draft + 1], n_accepted and draft_lens
+    device int32 [n_seq]."""
+    n_seq, rows, vocab = target.shape
+    t_seq, t_pos, t_one = target.stride()
+    assert t_one == 1 or vocab == 1
+    assert uniforms.is_contiguous() and uniforms.shape == (n_seq, rows) and _dtype_code(uniforms) == DTYPE_F32
+    assert tokens_out.shape == (n_seq, rows) and (rows == 1 or draft_tokens.shape == (n_seq, rows - 1))
+    _check_ints((draft_tokens, 0), (draft_lens, n_seq), (tokens_out, 1), (n_accepted, n_seq))
+    q_args = (None, 0, 0)
+    if draft is not None and rows > 1:
+        q_seq, q_pos, q_one = draft.stride()
+        assert draft.shape == (n_seq, rows - 1, vocab) and draft.dtype == target.dtype and (q_one == 1 or vocab == 1)
+        q_args = (draft.data_ptr(), q_seq, q_pos)
+    code = load().octopus_verify_drafts(target.data_ptr(), _dtype_code(target), t_seq, t_pos, *q_args, _ptr(draft_tokens), _ptr(draft_lens),
+                                        uniforms.data_ptr(), n_seq, rows - 1, vocab, tokens_out.data_ptr(), n_accepted.data_ptr(),
+                                        workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream))
+    _check(code, "octopus_verify_drafts")
 
 
 def octopus_profile_events(before, after):

@@ -261,6 +261,22 @@ struct CopyCall {
 };
 int launch_pages_copy(const CopyCall &c, int32_t n_pools, void *stream);
 
+// Verification of drafted tokens (octopus_verify.hip).  draft, draft_lens may be NULL.
+constexpr int32_t kMostPieces = 256;    // of a row
+struct RowSums {
+    double whole, rest;     // of a piece: the target's probabilities, what is left of them
+};
+struct VerifyCall {
+    const void *target, *draft;
+    int64_t target_seq, target_pos, draft_seq, draft_pos;   // strides in elements
+    const int32_t *tokens, *draft_lens;
+    const float *uniforms;
+    int32_t *tokens_out, *accepted;
+    RowSums *sums;          // [n_seq][pieces]
+    int32_t n_seq, n_draft, vocab, piece, pieces, is_bf16;
+};
+int launch_verify(const VerifyCall &c, void *stream);
+
 // What the entry points outside octopus_host.cpp ask of it: a plan whose parts fit together, codebooks the encoder takes, and the
 // measurement events armed for this thread's next decode-attention call (forgotten by the asking).
 bool plan_well_formed(const octopus_plan_t &plan);
