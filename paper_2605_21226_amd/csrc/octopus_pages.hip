@@ -7,46 +7,16 @@
 #include <hip/hip_runtime.h>
 
 #include "octopus_internal.h"
+#include "octopus_scan.hpp"
 
 namespace octopus {
 namespace {
 
-constexpr int kLanes = 64;
-
-// Inclusive sum over a wavefront's lanes.
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-    for (int m = 1; m < kLanes; m *= 2) {
-        const int other = __shfl_up(x, m, kLanes);
-        x += lane >= m ? other : 0;
-    }
-    return x;
-}
-
-// Exclusive sums over a workgroup's threads, and everybody's sum.  (all threads call this; `room` is free again after the next barrier)
-template <int THREADS>
-__device__ __forceinline__ int block_scan(int x, int *room, int *total) {
-    constexpr int WAVES = THREADS / kLanes;
-    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
-    const int upto = wave_scan(x, lane);
-    __syncthreads();
-    if (lane == kLanes - 1) room[wave] = upto;
-    __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        const int n = room[w];
-        before += w < wave ? n : 0;
-        all += n;
-    }
-    *total = all;
-    return before + upto - x;
-}
-
 __device__ __forceinline__ int pages_of(int tokens) { return (tokens + (OCTOPUS_TILE - 1)) / OCTOPUS_TILE; }
 __device__ __forceinline__ int page_id(const PagesCall &c, int id) { return min(max(id, 0), c.n_pages - 1); }
-// (counts change under atomics of this launch: a read goes to where those happen)
-__device__ __forceinline__ int32_t load_count(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Counts that one workgroup changes and reads; a barrier stands between.  (A fence for the whole device takes microseconds each.)
+__device__ __forceinline__ int32_t load_count(const int32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void add_count(int32_t *p, int n) { __hip_atomic_fetch_add(p, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
 // What a slot has, keeps and is to have.
 struct Slot {
@@ -68,36 +38,109 @@ __device__ __forceinline__ Slot slot_of(const PagesCall &c, int s) {
 }
 
 // Rows that come from another slot: what they keep is set aside (the row that it comes from may change too), and the counts follow.  A
-// thread per entry.
-constexpr int kRowThreads = 256;
+// thread has one entry of kShareSlots slots, whose reads are on their way at once; slots of one source that follow each other add to a page's
+// count together (64 samples of a prompt of 1024 pages: 27.3 us with an atomic addition a slot, SHARE_US so).
+constexpr int kRowThreads = 256, kShareSlots = 16;
 __global__ __launch_bounds__(kRowThreads) void pages_share_kernel(PagesCall c) {
-    const int s = blockIdx.y, j = blockIdx.x * kRowThreads + threadIdx.x;
-    const Slot x = slot_of(c, s);
-    const int kept = pages_of(x.kept), own = pages_of(x.own);
-    const int64_t row = static_cast<int64_t>(s) * c.max_pages;
-    const bool moved = x.src != s;
-    if (j < own && (moved || j >= kept)) atomicAdd(&c.refs[page_id(c, c.table[row + j])], -1);
-    if (moved && j < kept) {
-        const int page = page_id(c, c.table[static_cast<int64_t>(x.src) * c.max_pages + j]);
-        c.staged[row + j] = page;
-        atomicAdd(&c.refs[page], 1);
+    __shared__ Slot slots[kShareSlots];
+    const int s0 = blockIdx.y * kShareSlots, j = blockIdx.x * kRowThreads + threadIdx.x;
+    if (threadIdx.x < kShareSlots) slots[threadIdx.x] = s0 + static_cast<int>(threadIdx.x) < c.n_seq ? slot_of(c, s0 + threadIdx.x) : Slot{-1, 0, 0, 0};
+    __syncthreads();
+    int32_t lost[kShareSlots], taken[kShareSlots];     // page ids, -1: none
+#pragma unroll
+    for (int i = 0; i < kShareSlots; ++i) {            // (every read is of an entry that is there, so that none waits for a branch)
+        const Slot x = slots[i];
+        const int64_t own = static_cast<int64_t>(s0 + i) * c.max_pages + j, from = static_cast<int64_t>(x.src) * c.max_pages + j;
+        lost[i] = c.table[j < pages_of(x.own) ? own : 0];
+        taken[i] = c.table[x.src >= 0 && j < pages_of(x.kept) ? from : 0];
+    }
+#pragma unroll
+    for (int i = 0; i < kShareSlots; ++i) {
+        const Slot x = slots[i];
+        const bool moved = x.src != s0 + i;
+        lost[i] = j < pages_of(x.own) && (moved || j >= pages_of(x.kept)) ? page_id(c, lost[i]) : -1;
+        taken[i] = moved && j < pages_of(x.kept) ? page_id(c, taken[i]) : -1;
+    }
+    int less = 0, more = 0;
+#pragma unroll
+    for (int i = 0; i < kShareSlots; ++i) {
+        if (taken[i] >= 0) c.staged[static_cast<int64_t>(s0 + i) * c.max_pages + j] = taken[i];
+        const bool stays = lost[i] == taken[i];        // (a slot that comes from one whose page it held already)
+        if (lost[i] >= 0) {
+            less += stays ? 0 : 1;
+            if (less != 0 && (i + 1 == kShareSlots || lost[i + 1] != lost[i])) {
+                atomicAdd(&c.refs[lost[i]], -less);
+                less = 0;
+            }
+        }
+        if (taken[i] >= 0) {
+            more += stays ? 0 : 1;
+            if (more != 0 && (i + 1 == kShareSlots || taken[i + 1] != taken[i])) {
+                atomicAdd(&c.refs[taken[i]], more);
+                more = 0;
+            }
+        }
     }
 }
 
-// Which pages are copied, which free pages go where: one workgroup, a thread per slot, in rounds of as many slots.
-constexpr int kAssignThreads = 1024;
-constexpr int kPerThread = 16;       // counts a thread reads at once in the search
-__global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall c) {
-    __shared__ int room[kAssignThreads / kLanes];
-    __shared__ int first_of[kAssignThreads], entry_of[kAssignThreads];
-    const int tid = threadIdx.x;
+// Pages of `at` .. `at` + kPerThread - 1 that are free (bits).
+constexpr int kPerThread = 16;
+__device__ __forceinline__ uint32_t free_pages(const PagesCall &c, int64_t at) {
+    uint32_t free = 0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; i += 4) {
+        if (at + i + 4 <= c.n_pages) {
+            const int4 n = *reinterpret_cast<const int4 *>(c.refs + at + i);
+            free |= ((n.x <= 0 ? 1u : 0u) | (n.y <= 0 ? 2u : 0u) | (n.z <= 0 ? 4u : 0u) | (n.w <= 0 ? 8u : 0u)) << i;
+        } else {
+            for (int k = i; k < i + 4; ++k)
+                if (at + k < c.n_pages && c.refs[at + k] <= 0) free |= 1u << k;
+        }
+    }
+    return free;
+}
 
-    // f(slot, k, n): the k-th of the slot's `count` items, the n-th of this round; any thread, all of them at once
-    auto each = [&](int base, int count, int entry, auto f) {
+// Which pages are copied, which free pages go where: one workgroup, a thread per slot; more slots than threads (ONE false) in rounds of
+// as many.  Its time is that of reads that wait for each other: the slots' lengths, their entries, the counts of those (and the first
+// counts of the search), and the barriers between.
+constexpr int kAssignThreads = 1024;
+constexpr int kFew = 4;              // entries of a slot that its thread deals with by itself
+// With few entries in all (ROWS) it takes the rows from their sources as well, kEntries entries a thread, which wait in registers until all
+// rows have been read.
+constexpr int kEntries = 8;
+template <bool ONE, bool ROWS>
+__global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall c) {
+    static_assert(ONE || !ROWS, "rows are looked up by a thread per slot");
+    __shared__ int room[2][kAssignThreads / kScanLanes];
+    __shared__ int first_of[kAssignThreads], entry_of[kAssignThreads], fresh[kAssignThreads];
+    __shared__ int flags[4];
+    const int tid = threadIdx.x;
+    if (tid < 4) flags[tid] = 0;
+    __syncthreads();
+    // whether it holds for any thread, in this round or one before (all threads call it; a barrier)
+    auto any = [&](int which, bool it) {
+        if (it) flags[which] = 1;
+        __syncthreads();
+        const bool is = flags[which] != 0;
+        if constexpr (!ONE) __syncthreads();     // (the next round may set it)
+        return is;
+    };
+    SlotPages mine{0, 0, -1, 0};         // ONE: the thread's slot
+    auto slot = [&](int s) { return ONE ? mine : c.info[s]; };
+    auto set_copied = [&](int s) {
+        if constexpr (ONE) mine.copied = 1;
+        else c.info[s].copied = 1;
+    };
+    __shared__ Slot slots[ROWS ? kAssignThreads : 1];
+    __shared__ int page_in[ROWS ? kAssignThreads : 1], pages_stay[ROWS ? kAssignThreads : 1];
+    int32_t row[kEntries];               // ROWS: what the thread's entries become, -1: nothing new
+    const int n_entries = ROWS ? c.n_seq * c.max_pages : 0;
+
+    // f(slot, k, entry, n): the k-th of the slot's `count` items, the n-th of this round; by all threads, whosever they are
+    auto spread = [&](int base, int count, int entry, auto f) {
         int total;
-        const int before = block_scan<kAssignThreads>(count, room, &total);
-        if (total == 0) return;
-        first_of[tid] = before;
+        const int upto = block_scan<kAssignThreads>(count, room[0], &total);
+        first_of[tid] = upto - count;
         entry_of[tid] = entry;
         __syncthreads();
         for (int n = tid; n < total; n += kAssignThreads) {
@@ -116,17 +159,21 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
         int lost = 0, from = 0;
         if (s < c.n_seq) {
             const Slot x = slot_of(c, s);
-            c.info[s] = SlotPages{x.kept, x.want, x.src, 0};
+            const SlotPages kept{x.kept, x.want, x.src, 0};
+            if constexpr (ONE) mine = kept;
+            else c.info[s] = kept;
             from = pages_of(x.kept);
-            lost = max(pages_of(x.own) - from, 0);
+            if (c.source == nullptr) lost = max(pages_of(x.own) - from, 0);
+            if constexpr (ROWS) slots[tid] = x;
         }
-        if (c.source == nullptr)
-            each(base, lost, from, [&](int slot, int k, int entry, int) {
-                atomicAdd(&c.refs[page_id(c, c.table[static_cast<int64_t>(slot) * c.max_pages + entry + k])], -1);
-            });
+        if (c.source != nullptr) continue;
+        auto lose = [&](int of, int k, int entry, int) {
+            add_count(&c.refs[page_id(c, c.table[static_cast<int64_t>(of) * c.max_pages + entry + k])], -1);
+        };
+        if (any(0, lost > kFew)) spread(base, lost, from, lose);
+        else
+            for (int k = 0; k < lost; ++k) lose(s, k, from, 0);
     }
-    __threadfence();
-    __syncthreads();
 
     // A page that is written into, because what a slot keeps ends inside it, has to be the slot's own.  Of those that would write into the same
     // one, the lowest keeps it if nobody else holds it -- one that continues its own row before those that came to it -- and the others
@@ -136,101 +183,139 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
         return x.want > x.kept && x.kept % OCTOPUS_TILE != 0 ? page_id(c, x.src == s ? c.table[at] : c.staged[at]) : -1;
     };
     auto rank = [&](int s, const SlotPages &x) { return x.src == s ? s : c.n_seq + s; };
+    int my_page = -1;                    // ONE: the page that the thread's slot writes into
+    if constexpr (ROWS) {
+        __syncthreads();
+        int32_t lost[kEntries];
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {           // (every read is of an entry that is there)
+            const int e = min(tid + i * kAssignThreads, n_entries - 1), s = e / c.max_pages, j = e - s * c.max_pages;
+            const Slot x = slots[s];
+            lost[i] = c.table[e];
+            row[i] = c.table[x.src >= 0 ? x.src * c.max_pages + j : e];
+        }
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {
+            const int e = tid + i * kAssignThreads, s = min(e, n_entries - 1) / c.max_pages, j = e - s * c.max_pages;
+            const Slot x = slots[s];
+            const bool there = e < n_entries, moved = x.src != s, keeps = there && j < pages_of(x.kept);
+            lost[i] = there && j < pages_of(x.own) && (moved || !keeps) ? page_id(c, lost[i]) : -1;
+            if (keeps && j == x.kept / OCTOPUS_TILE) page_in[s] = page_id(c, row[i]);
+            row[i] = keeps && moved ? page_id(c, row[i]) : -1;
+            if (lost[i] != row[i]) {                   // (a slot that comes from one whose page it held already: no change)
+                if (lost[i] >= 0) add_count(&c.refs[lost[i]], -1);
+                if (row[i] >= 0) add_count(&c.refs[row[i]], 1);
+            }
+        }
+        __syncthreads();
+        if (tid < c.n_seq && mine.want > mine.kept && mine.kept % OCTOPUS_TILE != 0) my_page = page_in[tid];
+    } else if constexpr (ONE) {
+        if (tid < c.n_seq) my_page = written(tid, mine);
+    }
+    auto page_of = [&](int s) { return ONE ? my_page : written(s, c.info[s]); };
+    __syncthreads();
+    uint32_t free = free_pages(c, tid * kPerThread);
     bool shared = false;
     for (int s = tid; s < c.n_seq; s += kAssignThreads) {
-        const int page = written(s, c.info[s]);
+        const int page = page_of(s);
         shared |= page >= 0 && load_count(&c.refs[page]) > 1;
     }
-    if (__syncthreads_or(shared)) {
+    if (any(1, shared)) {
         for (int s = tid; s < c.n_seq; s += kAssignThreads) {
-            const int page = written(s, c.info[s]);
+            const int page = page_of(s);
             if (page >= 0) {
                 c.writers[page] = 0;
                 c.first[page] = INT32_MAX;
             }
         }
-        __threadfence();
         __syncthreads();
         for (int s = tid; s < c.n_seq; s += kAssignThreads) {
-            const SlotPages x = c.info[s];
-            const int page = written(s, x);
+            const int page = page_of(s);
             if (page >= 0) {
-                atomicAdd(&c.writers[page], 1);
-                atomicMin(&c.first[page], rank(s, x));
+                add_count(&c.writers[page], 1);
+                __hip_atomic_fetch_min(&c.first[page], rank(s, slot(s)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             }
         }
-        __threadfence();
         __syncthreads();
         for (int s = tid; s < c.n_seq; s += kAssignThreads) {
-            const SlotPages x = c.info[s];
-            const int page = written(s, x);
-            if (page >= 0 && (load_count(&c.refs[page]) > load_count(&c.writers[page]) || load_count(&c.first[page]) != rank(s, x)))
-                c.info[s].copied = 1;
+            const int page = page_of(s);
+            if (page >= 0 && (load_count(&c.refs[page]) > load_count(&c.writers[page]) || load_count(&c.first[page]) != rank(s, slot(s)))) set_copied(s);
         }
     }
 
     // pages that are asked for
     auto asked = [&](const SlotPages &x) { return x.want > x.kept ? pages_of(x.want) - pages_of(x.kept) + x.copied : 0; };
     int wanted = 0, copies = 0;
+    int my_upto = 0;                     // ONE: pages asked for up to the thread's slot
     for (int base = 0; base < c.n_seq; base += kAssignThreads) {
-        const int s = base + tid;
-        const SlotPages x = s < c.n_seq ? c.info[s] : SlotPages{0, 0, 0, 0};
         int total;
-        block_scan<kAssignThreads>(asked(x), room, &total);
+        my_upto = block_scan<kAssignThreads>(base + tid < c.n_seq ? asked(slot(base + tid)) : 0, room[0], &total);
         wanted += total;
     }
 
     // the lowest free ones, in order
+    const bool in_lds = wanted <= kAssignThreads;
     int found = 0;
     for (int64_t base = 0; found < wanted && base < c.n_pages; base += kAssignThreads * kPerThread) {
         const int64_t at = base + tid * kPerThread;
-        uint32_t free = 0;
-        if (at + kPerThread <= c.n_pages) {
-            int4 n[kPerThread / 4];
-#pragma unroll
-            for (int i = 0; i < kPerThread / 4; ++i) n[i] = *reinterpret_cast<const int4 *>(c.refs + at + 4 * i);
-#pragma unroll
-            for (int i = 0; i < kPerThread / 4; ++i)
-                free |= ((n[i].x <= 0 ? 1u : 0u) | (n[i].y <= 0 ? 2u : 0u) | (n[i].z <= 0 ? 4u : 0u) | (n[i].w <= 0 ? 8u : 0u)) << (4 * i);
-        } else {
-            for (int i = 0; i < kPerThread; ++i)
-                if (at + i < c.n_pages && c.refs[at + i] <= 0) free |= 1u << i;
-        }
+        if (base != 0) free = free_pages(c, at);
         int total;
-        int n = found + block_scan<kAssignThreads>(__popc(free), room, &total);
-        for (; free != 0 && n < wanted; free &= free - 1, ++n) c.fresh[n] = static_cast<int32_t>(at) + __ffs(free) - 1;
+        int n = found + block_scan<kAssignThreads>(static_cast<int>(__popc(free)), room[1], &total) - static_cast<int>(__popc(free));
+        for (; free != 0 && n < wanted; free &= free - 1, ++n) {
+            const int page = static_cast<int>(at) + __ffs(free) - 1;
+            if (in_lds) fresh[n] = page;
+            else c.fresh[n] = page;
+        }
         found += total;
     }
     const bool enough = found >= wanted;
-    __threadfence();
     __syncthreads();
+    auto fresh_page = [&](int n) { return in_lds ? fresh[n] : c.fresh[n]; };
 
     int given = 0;
     for (int base = 0; base < c.n_seq; base += kAssignThreads) {
         const int s = base + tid;
-        SlotPages x = s < c.n_seq ? c.info[s] : SlotPages{0, 0, 0, 0};
-        const int need = enough ? asked(x) : 0;
+        SlotPages x = s < c.n_seq ? slot(s) : SlotPages{0, 0, 0, 0};
         if (!enough) x.copied = 0;
-        int total, moved;
-        const int begin = given + block_scan<kAssignThreads>(need, room, &total);
-        const int nth = copies + block_scan<kAssignThreads>(x.copied, room, &moved);
-        if (x.copied != 0) {
-            const int page = written(s, x);
-            c.moves[2 + 2 * nth] = page;
-            c.moves[3 + 2 * nth] = c.fresh[begin];
-            atomicAdd(&c.refs[page], -1);
-        }
-        each(base, need, pages_of(x.kept) - x.copied, [&](int slot, int k, int entry, int n) {   // (a barrier stands before its writes)
-            const int page = c.fresh[given + n];
-            c.table[static_cast<int64_t>(slot) * c.max_pages + entry + k] = page;
-            c.refs[page] = 1;
-        });
         if (s < c.n_seq) {
             c.lens[s] = enough ? x.want : x.kept;
-            c.info[s] = x;
+            if (!ROWS && (!ONE || c.source != nullptr)) c.info[s] = x;
+            if constexpr (ROWS) pages_stay[s] = pages_of(x.kept) - x.copied;
         }
+        if (!enough || wanted == 0) continue;
+        const int need = asked(x);
+        int total = wanted, upto = my_upto, moved;
+        if constexpr (!ONE) upto = block_scan<kAssignThreads>(need, room[0], &total);
+        const int begin = given + upto - need;
+        if (any(2, x.copied != 0)) {
+            const int nth = copies + block_scan<kAssignThreads>(x.copied, room[1], &moved) - x.copied;
+            if (x.copied != 0) {
+                const int page = ONE ? my_page : written(s, x);
+                c.moves[2 + 2 * nth] = page;
+                c.moves[3 + 2 * nth] = fresh_page(begin);
+                add_count(&c.refs[page], -1);
+            }
+            copies += moved;
+        }
+        auto give = [&](int of, int k, int entry, int n) {
+            const int page = fresh_page(n);
+            c.table[static_cast<int64_t>(of) * c.max_pages + entry + k] = page;
+            c.refs[page] = 1;
+        };
+        const int entry = pages_of(x.kept) - x.copied;
+        if (any(3, need > kFew))    // (a barrier stands between the reads of entries above and these writes)
+            spread(base, need, entry, [&](int of, int k, int first, int n) { give(of, k, first, given + n); });
+        else
+            for (int k = 0; k < need; ++k) give(s, k, entry, begin + k);
         given += total;
-        copies += moved;
+    }
+    if constexpr (ROWS) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {
+            const int e = tid + i * kAssignThreads;
+            if (row[i] >= 0 && e % c.max_pages < pages_stay[e / c.max_pages]) c.table[e] = row[i];     // (a copied page's entry has been written)
+        }
     }
     if (tid == 0) {
         c.moves[0] = copies;
@@ -251,30 +336,21 @@ __global__ __launch_bounds__(kRowThreads) void pages_rows_kernel(PagesCall c) {
 // from n on go below n; after it the pages in use are 0 .. n - 1.  A workgroup counts its pages, and then numbers them from the others' counts.
 constexpr int kCountThreads = 256;
 constexpr int kCounted = kCountThreads * kPerThread;   // pages a workgroup looks at
+// (pages past the last are neither in use nor free)
 __device__ __forceinline__ uint32_t used_pages(const PagesCall &c, int64_t at) {
-    uint32_t used = 0;
-#pragma unroll
-    for (int i = 0; i < kPerThread; i += 4) {
-        if (at + i + 4 <= c.n_pages) {
-            const int4 n = *reinterpret_cast<const int4 *>(c.refs + at + i);
-            used |= ((n.x > 0 ? 1u : 0u) | (n.y > 0 ? 2u : 0u) | (n.z > 0 ? 4u : 0u) | (n.w > 0 ? 8u : 0u)) << i;
-        } else {
-            for (int k = i; k < i + 4; ++k)
-                if (at + k < c.n_pages && c.refs[at + k] > 0) used |= 1u << k;
-        }
-    }
-    return used;
+    const int64_t there = min(max(c.n_pages - at, static_cast<int64_t>(0)), static_cast<int64_t>(kPerThread));
+    return ~free_pages(c, at) & ((1u << there) - 1u);
 }
 
 __global__ __launch_bounds__(kCountThreads) void pages_count_kernel(PagesCall c) {
-    __shared__ int room[kCountThreads / kLanes];
+    __shared__ int room[kCountThreads / kScanLanes];
     int total;
-    block_scan<kCountThreads>(__popc(used_pages(c, static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread)), room, &total);
+    block_scan<kCountThreads>(static_cast<int>(__popc(used_pages(c, static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread))), room, &total);
     if (threadIdx.x == 0) c.writers[blockIdx.x] = total;
 }
 
 __global__ __launch_bounds__(kCountThreads) void pages_pair_kernel(PagesCall c) {
-    __shared__ int room[kCountThreads / kLanes];
+    __shared__ int room[kCountThreads / kScanLanes];
     int before = 0, all = 0;
     for (int b = threadIdx.x; b < static_cast<int>(gridDim.x); b += kCountThreads) {
         const int n = c.writers[b];
@@ -286,7 +362,7 @@ __global__ __launch_bounds__(kCountThreads) void pages_pair_kernel(PagesCall c) 
     block_scan<kCountThreads>(before, room, &n_before);
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread;
     const uint32_t used = used_pages(c, at);
-    int n = n_before + block_scan<kCountThreads>(__popc(used), room, &total);    // pages in use below this one
+    int n = n_before + block_scan<kCountThreads>(static_cast<int>(__popc(used)), room, &total) - static_cast<int>(__popc(used));    // pages in use below this one
     for (int i = 0; i < kPerThread; ++i) {
         const int id = static_cast<int>(at) + i;
         if (id >= c.n_pages) break;
@@ -351,9 +427,17 @@ dim3 row_grid(const PagesCall &c) { return dim3((c.max_pages + kRowThreads - 1) 
 
 int launch_pages_update(const PagesCall &c, void *stream) {
     const hipStream_t on = static_cast<hipStream_t>(stream);
-    if (c.source != nullptr) hipLaunchKernelGGL(pages_share_kernel, row_grid(c), dim3(kRowThreads), 0, on, c);
-    hipLaunchKernelGGL(pages_assign_kernel, dim3(1), dim3(kAssignThreads), 0, on, c);
-    if (c.source != nullptr) hipLaunchKernelGGL(pages_rows_kernel, row_grid(c), dim3(kRowThreads), 0, on, c);
+    const dim3 rows = row_grid(c);
+    const bool one = c.n_seq <= kAssignThreads, few = one && static_cast<int64_t>(c.n_seq) * c.max_pages <= kEntries * kAssignThreads;
+    auto assign = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(1), dim3(kAssignThreads), 0, on, c); };
+    if (c.source != nullptr && few) {
+        assign(pages_assign_kernel<true, true>);
+        return static_cast<int>(hipGetLastError());
+    }
+    if (c.source != nullptr) hipLaunchKernelGGL(pages_share_kernel, dim3(rows.x, (c.n_seq + kShareSlots - 1) / kShareSlots), dim3(kRowThreads), 0, on, c);
+    if (one) assign(pages_assign_kernel<true, false>);
+    else assign(pages_assign_kernel<false, false>);
+    if (c.source != nullptr) hipLaunchKernelGGL(pages_rows_kernel, rows, dim3(kRowThreads), 0, on, c);
     return static_cast<int>(hipGetLastError());
 }
 

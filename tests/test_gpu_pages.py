@@ -90,7 +90,8 @@ def server(n_seq, per, n_pages, lens, seed=0, **more):
     return Server(refs, table, lens, **more)
 
 
-@pytest.mark.parametrize("n_seq,per,n_pages", [(1, 1, 1), (1, 3, 5), (7, 4, 40), (64, 9, 700), (300, 5, 1600), (1500, 3, 5000)])
+@pytest.mark.parametrize("n_seq,per,n_pages", [(1, 1, 1), (1, 3, 5), (7, 4, 40), (64, 9, 700), (1024, 8, 9000), (1024, 9, 5000), (33, 300, 9000),
+                                               (1025, 2, 3000), (2100, 3, 7000)])
 @pytest.mark.parametrize("with_source", [False, True])
 def test_steps(n_seq, per, n_pages, with_source):
     """Growth, trims, forks, slots that move, end and begin, at random, one after the other, until pages run out and after."""
