@@ -39,7 +39,7 @@ __device__ __forceinline__ Slot slot_of(const PagesCall &c, int s) {
 
 // Rows that come from another slot: what they keep is set aside (the row that it comes from may change too), and the counts follow.  A
 // thread has one entry of kShareSlots slots, whose reads are on their way at once; slots of one source that follow each other add to a page's
-// count together (64 samples of a prompt of 1024 pages: 27.3 us with an atomic addition a slot, SHARE_US so).
+// count together (64 samples of a prompt of 1024 pages: 27.3 us with an atomic addition a slot, 8.4 so).
 constexpr int kRowThreads = 256, kShareSlots = 16;
 __global__ __launch_bounds__(kRowThreads) void pages_share_kernel(PagesCall c) {
     __shared__ Slot slots[kShareSlots];
@@ -184,19 +184,25 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
     };
     auto rank = [&](int s, const SlotPages &x) { return x.src == s ? s : c.n_seq + s; };
     int my_page = -1;                    // ONE: the page that the thread's slot writes into
+    // (entry e of the table is entry j of slot s; the quotient's error is far below the half that is added, e < 2^13)
+    const float per_entry = 1.0f / c.max_pages;
+    auto slot_at = [&](int e) { return static_cast<int>((e + 0.5f) * per_entry); };
     if constexpr (ROWS) {
+        static_assert(kEntries * kAssignThreads <= 1 << 13, "");
         __syncthreads();
         int32_t lost[kEntries];
 #pragma unroll
         for (int i = 0; i < kEntries; ++i) {           // (every read is of an entry that is there)
-            const int e = min(tid + i * kAssignThreads, n_entries - 1), s = e / c.max_pages, j = e - s * c.max_pages;
+            if (i * kAssignThreads >= n_entries) break;
+            const int e = min(tid + i * kAssignThreads, n_entries - 1), s = slot_at(e), j = e - s * c.max_pages;
             const Slot x = slots[s];
             lost[i] = c.table[e];
             row[i] = c.table[x.src >= 0 ? x.src * c.max_pages + j : e];
         }
 #pragma unroll
         for (int i = 0; i < kEntries; ++i) {
-            const int e = tid + i * kAssignThreads, s = min(e, n_entries - 1) / c.max_pages, j = e - s * c.max_pages;
+            if (i * kAssignThreads >= n_entries) break;
+            const int e = tid + i * kAssignThreads, s = slot_at(min(e, n_entries - 1)), j = e - s * c.max_pages;
             const Slot x = slots[s];
             const bool there = e < n_entries, moved = x.src != s, keeps = there && j < pages_of(x.kept);
             lost[i] = there && j < pages_of(x.own) && (moved || !keeps) ? page_id(c, lost[i]) : -1;
@@ -313,8 +319,9 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kEntries; ++i) {
-            const int e = tid + i * kAssignThreads;
-            if (row[i] >= 0 && e % c.max_pages < pages_stay[e / c.max_pages]) c.table[e] = row[i];     // (a copied page's entry has been written)
+            if (i * kAssignThreads >= n_entries) break;
+            const int e = tid + i * kAssignThreads, s = slot_at(min(e, n_entries - 1));
+            if (row[i] >= 0 && e - s * c.max_pages < pages_stay[s]) c.table[e] = row[i];     // (a copied page's entry has been written)
         }
     }
     if (tid == 0) {
@@ -333,19 +340,71 @@ __global__ __launch_bounds__(kRowThreads) void pages_rows_kernel(PagesCall c) {
 }
 
 // Compaction: with n pages in use, the i-th highest of them goes to the i-th lowest free page as long as that is lower, that is, those
-// from n on go below n; after it the pages in use are 0 .. n - 1.  A workgroup counts its pages, and then numbers them from the others' counts.
-constexpr int kCountThreads = 256;
-constexpr int kCounted = kCountThreads * kPerThread;   // pages a workgroup looks at
+// from n on go below n; after it the pages in use are 0 .. n - 1.
 // (pages past the last are neither in use nor free)
 __device__ __forceinline__ uint32_t used_pages(const PagesCall &c, int64_t at) {
     const int64_t there = min(max(c.n_pages - at, static_cast<int64_t>(0)), static_cast<int64_t>(kPerThread));
     return ~free_pages(c, at) & ((1u << there) - 1u);
 }
+// Pages from `at` on, of which `used` are in use and `n` below them: their places in `moves`, and in the map those of the pages that stay.
+__device__ __forceinline__ void pair_pages(const PagesCall &c, int64_t at, uint32_t used, int n, int n_used) {
+    for (int i = 0; i < kPerThread; ++i) {
+        const int id = static_cast<int>(at) + i;
+        if (id >= c.n_pages) break;
+        const bool is = (used >> i) & 1u;
+        if (is && id >= n_used) c.moves[2 + 2 * (n_used - 1 - n)] = id;
+        else c.page_map[id] = id;
+        if (!is && id < n_used) c.moves[3 + 2 * (id - n)] = id;
+        n += is ? 1 : 0;
+        if (id == n_used - 1) c.moves[0] = n_used - n;      // free pages below n_used
+    }
+    if (at == 0) {
+        c.moves[1] = n_used;
+        if (n_used == 0) c.moves[0] = 0;
+    }
+}
+__device__ __forceinline__ void apply_move(const PagesCall &c, int i) {
+    const int from = c.moves[2 + 2 * i], to = c.moves[3 + 2 * i];
+    c.refs[to] = c.refs[from];
+    c.refs[from] = 0;
+    c.page_map[from] = to;
+}
 
+// Pools of up to 65536 pages: one workgroup (three launches of the form below took 8.3 us for 1100 pages, this one 6.1).
+constexpr int kCompactRounds = 4;
+__global__ __launch_bounds__(kAssignThreads) void pages_compact_kernel(PagesCall c) {
+    __shared__ int room[kAssignThreads / kScanLanes];
+    const int tid = threadIdx.x;
+    uint32_t used[kCompactRounds];
+    int below[kCompactRounds], n_used = 0;
+#pragma unroll
+    for (int r = 0; r < kCompactRounds; ++r) used[r] = used_pages(c, (r * kAssignThreads + tid) * kPerThread);
+#pragma unroll
+    for (int r = 0; r < kCompactRounds; ++r) {
+        if (r * kAssignThreads * kPerThread >= c.n_pages) break;
+        int total;
+        const int n = static_cast<int>(__popc(used[r]));
+        below[r] = n_used + block_scan<kAssignThreads>(n, room, &total) - n;
+        n_used += total;
+    }
+#pragma unroll
+    for (int r = 0; r < kCompactRounds; ++r) {
+        if (r * kAssignThreads * kPerThread >= c.n_pages) break;
+        pair_pages(c, (r * kAssignThreads + tid) * kPerThread, used[r], below[r], n_used);
+    }
+    __syncthreads();
+    const int n = __hip_atomic_load(c.moves, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    for (int i = tid; i < n; i += kAssignThreads) apply_move(c, i);
+}
+
+// More pages: a workgroup counts its pages, and then numbers them from the others' counts.
+constexpr int kCountThreads = 256;
+constexpr int kCounted = kCountThreads * kPerThread;   // pages a workgroup looks at
 __global__ __launch_bounds__(kCountThreads) void pages_count_kernel(PagesCall c) {
     __shared__ int room[kCountThreads / kScanLanes];
+    const uint32_t used = used_pages(c, static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread);
     int total;
-    block_scan<kCountThreads>(static_cast<int>(__popc(used_pages(c, static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread))), room, &total);
+    block_scan<kCountThreads>(static_cast<int>(__popc(used)), room, &total);
     if (threadIdx.x == 0) c.writers[blockIdx.x] = total;
 }
 
@@ -362,30 +421,13 @@ __global__ __launch_bounds__(kCountThreads) void pages_pair_kernel(PagesCall c) 
     block_scan<kCountThreads>(before, room, &n_before);
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kCounted + threadIdx.x * kPerThread;
     const uint32_t used = used_pages(c, at);
-    int n = n_before + block_scan<kCountThreads>(static_cast<int>(__popc(used)), room, &total) - static_cast<int>(__popc(used));    // pages in use below this one
-    for (int i = 0; i < kPerThread; ++i) {
-        const int id = static_cast<int>(at) + i;
-        if (id >= c.n_pages) break;
-        const bool is = (used >> i) & 1u;
-        c.page_map[id] = id;
-        if (is && id >= n_used) c.moves[2 + 2 * (n_used - 1 - n)] = id;
-        if (!is && id < n_used) c.moves[3 + 2 * (id - n)] = id;
-        n += is ? 1 : 0;
-        if (id == n_used - 1) c.moves[0] = n_used - n;      // free pages below n_used
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        c.moves[1] = n_used;
-        if (n_used == 0) c.moves[0] = 0;
-    }
+    const int n = static_cast<int>(__popc(used));
+    pair_pages(c, at, used, n_before + block_scan<kCountThreads>(n, room, &total) - n, n_used);
 }
 
 __global__ __launch_bounds__(kCountThreads) void pages_apply_kernel(PagesCall c) {
     const int i = blockIdx.x * kCountThreads + threadIdx.x;
-    if (i >= c.moves[0]) return;
-    const int from = c.moves[2 + 2 * i], to = c.moves[3 + 2 * i];
-    c.refs[to] = c.refs[from];
-    c.refs[from] = 0;
-    c.page_map[from] = to;
+    if (i < c.moves[0]) apply_move(c, i);
 }
 
 __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(PagesCall c) {
@@ -396,10 +438,14 @@ __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(PagesCall c) 
     c.table[at] = c.page_map[page_id(c, c.table[at])];
 }
 
-// A pool's pages by blockIdx.y, pieces of 16 KB of the moved pages by blockIdx.x.
+// A pool's pages by blockIdx.y, pieces of 16 KB of the moved pages by blockIdx.x.  What is written streams past the caches, what is read
+// does not, since samples of one prompt all read its last page.  Pages at random places, keys and values of eight kv heads at d = 128, 3 bits:
+// 32 pages of eight layers (84 MB read and written) 28 us with ordinary stores, 16.5 with streaming ones, 63 copies of one page of sixteen 50 and 37,
+// 141 pages of eight layers (370 MB) 93 and 82, 4.5 TB/s, where a copy of as much in one piece reaches 5.3; streaming reads too: 21, 57 and 83.
 constexpr int kCopyThreads = 256, kCopyAhead = 4;
 constexpr int kPieceWords = kCopyThreads * kCopyAhead;     // of 16 bytes
 __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(CopyCall c) {
+    typedef uint32_t word_t __attribute__((ext_vector_type(4)));
     const CopyPool pool = c.pools[blockIdx.y];
     const int64_t words = pool.page_bytes / 16;
     const int pieces = static_cast<int>((words + kPieceWords - 1) / kPieceWords);
@@ -409,15 +455,15 @@ __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(CopyCall c) {
         const int64_t first = (i % pieces) * kPieceWords + threadIdx.x;
         const uint32_t from = c.moves[2 + 2 * move], to = c.moves[3 + 2 * move];
         if (from >= static_cast<uint32_t>(c.n_pages) || to >= static_cast<uint32_t>(c.n_pages)) continue;
-        const uint4 *src = static_cast<const uint4 *>(pool.data) + from * words;
-        uint4 *dst = static_cast<uint4 *>(pool.data) + to * words;
-        uint4 x[kCopyAhead];
+        const word_t *src = static_cast<const word_t *>(pool.data) + from * words;
+        word_t *dst = static_cast<word_t *>(pool.data) + to * words;
+        word_t x[kCopyAhead];
 #pragma unroll
         for (int k = 0; k < kCopyAhead; ++k)
             if (first + k * kCopyThreads < words) x[k] = src[first + k * kCopyThreads];
 #pragma unroll
         for (int k = 0; k < kCopyAhead; ++k)
-            if (first + k * kCopyThreads < words) dst[first + k * kCopyThreads] = x[k];
+            if (first + k * kCopyThreads < words) __builtin_nontemporal_store(x[k], &dst[first + k * kCopyThreads]);
     }
 }
 
@@ -443,6 +489,10 @@ int launch_pages_update(const PagesCall &c, void *stream) {
 
 int launch_pages_compact(const PagesCall &c, void *stream) {
     const hipStream_t on = static_cast<hipStream_t>(stream);
+    if (c.n_pages <= kCompactRounds * kAssignThreads * kPerThread) {
+        hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kAssignThreads), 0, on, c);
+        return static_cast<int>(hipGetLastError());
+    }
     const dim3 blocks((c.n_pages + kCounted - 1) / kCounted);
     hipLaunchKernelGGL(pages_count_kernel, blocks, dim3(kCountThreads), 0, on, c);
     hipLaunchKernelGGL(pages_pair_kernel, blocks, dim3(kCountThreads), 0, on, c);
@@ -461,7 +511,7 @@ int launch_pages_copy(const CopyCall &c, int32_t n_pools, void *stream) {
         const int64_t n = (c.pools[p].page_bytes / 16 + kPieceWords - 1) / kPieceWords;
         pieces = n > pieces ? n : pieces;
     }
-    const int64_t most = 4096 / n_pools, all = pieces * c.max_moves;
+    const int64_t most = 8192 / n_pools, all = pieces * c.max_moves;
     hipLaunchKernelGGL(pages_copy_kernel, dim3(static_cast<unsigned>(all < most ? all : most), n_pools), dim3(kCopyThreads), 0,
                        static_cast<hipStream_t>(stream), c);
     return static_cast<int>(hipGetLastError());

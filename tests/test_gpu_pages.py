@@ -212,7 +212,8 @@ def test_clamped_numbers():
     y.update([100])
 
 
-@pytest.mark.parametrize("n_pages,used", [(1, 0), (1, 1), (2, 1), (17, 9), (4096, 2000), (4097, 4096), (20000, 1), (70000, 35000), (70001, 70001)])
+@pytest.mark.parametrize("n_pages,used", [(1, 0), (1, 1), (2, 1), (17, 9), (4096, 2000), (16385, 9000), (20000, 1), (65536, 30000), (65537, 40000), (70001, 70001),
+                                          (200000, 90000)])
 def test_compaction(n_pages, used):
     rng = np.random.default_rng(n_pages + used)
     refs = np.zeros(n_pages, dtype=np.int64)
