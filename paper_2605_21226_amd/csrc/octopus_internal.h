@@ -273,9 +273,10 @@ struct VerifyCall {
     const float *uniforms;
     int32_t *tokens_out, *accepted;
     RowSums *sums;          // [n_seq][pieces]
-    int32_t n_seq, n_draft, vocab, piece, pieces, is_bf16;
+    int32_t n_seq, n_draft, vocab, is_bf16;
+    int32_t piece, pieces;  // set by the launcher
 };
-int launch_verify(const VerifyCall &c, void *stream);
+int launch_verify(VerifyCall c, void *stream);
 
 // What the entry points outside octopus_host.cpp ask of it: a plan whose parts fit together, codebooks the encoder takes, and the
 // measurement events armed for this thread's next decode-attention call (forgotten by the asking).

@@ -33,6 +33,15 @@ __device__ __forceinline__ T wave_scan(T x) {
     return x;
 }
 
+// x of one lane (the same for all), for all.
+__device__ __forceinline__ double wave_lane(double x, int lane) {
+    const long long b = __double_as_longlong(x);
+    const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(b), lane));
+    const unsigned hi = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane));
+    return __longlong_as_double(static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo));
+}
+__device__ __forceinline__ double wave_last(double x) { return wave_lane(x, kScanLanes - 1); }
+
 // Inclusive sums over a workgroup's threads, and everybody's.  All threads call it; `room` is free again after the next barrier.
 template <int THREADS, class T>
 __device__ __forceinline__ T block_scan(T x, T *room, T *total) {

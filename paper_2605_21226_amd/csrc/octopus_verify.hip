@@ -4,34 +4,62 @@
 // after them is drawn from the weights r = max(p_a - q_a, 0) if draft a fell (tokens come out distributed as the target's), from p_a
 // if all of them stand: the first token whose running sum of r exceeds u times the whole sum.
 //
-// A call reads a handful of numbers to find a, and then one row of each of the two distributions: memory bounds it for many sequences,
-// latency for few.  The row is cut into pieces, a workgroup each, that write their sums; a second launch finds the piece in which the
-// running sum gets there, and the token inside it.  Differences and sums are 64-bit numbers: u has 24 bits, and a running sum over
-// 10^5 tokens has to tell neighbours apart that differ by less.
+// A call reads a handful of numbers to find a, and then one row of each of the two distributions: memory bounds it for many sequences
+// (256 x 128256 tokens in fp32, 262 MB, 34 us), latency for few (1 x 8000 tokens 5.4 us, four reads that wait for each other).  A row is
+// cut into pieces, a wavefront each, that are summed; then a wavefront finds the piece in which the running sum gets there, reads it once
+// more and finds the token.  Differences and sums are 64-bit numbers: u has 24 bits, and a running sum over 10^5 tokens has to tell neighbours
+// apart that differ by less.  Rows that are subtracted from and rows that are not have code of their own, and pieces inside a row need no
+// comparison with its end: with both in one loop 1 x 8000 tokens took 7.8 us, 256 x 128256 40.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
 
 #include "octopus_internal.h"
+#include "octopus_scan.hpp"
 
 namespace octopus {
 namespace {
 
-constexpr int kLanes = 64, kThreads = 256, kWaves = kThreads / kLanes;
+constexpr int kLanes = kScanLanes;
 
 // A probability that counts: a positive finite number, or none.
-__device__ __forceinline__ float counted(float p) { return p > 0.0f && p < INFINITY ? p : 0.0f; }
+__device__ __forceinline__ float counted(float p) {
+    constexpr int kPositiveDenormal = 1 << 7, kPositiveNormal = 1 << 8;
+    return __builtin_amdgcn_classf(p, kPositiveDenormal | kPositiveNormal) ? p : 0.0f;
+}
 __device__ __forceinline__ double uniform(float u) { return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0; }   // [0, 1)
 
+// One of the distributions' rows.
 template <bool BF16>
 struct Row {
     using Word = typename std::conditional<BF16, uint16_t, float>::type;
-    static constexpr int AT_ONCE = 16 / sizeof(Word);      // of a 16-byte read
+    static constexpr int AT_ONCE = 16 / sizeof(Word);      // tokens of a 16-byte read
     const Word *p;
     __device__ __forceinline__ static Row of(const void *base, int64_t at) { return Row{static_cast<const Word *>(base) + at}; }
     __device__ __forceinline__ float operator[](int64_t i) const {
         if constexpr (BF16) return counted(__uint_as_float(static_cast<uint32_t>(p[i]) << 16));
         else return counted(p[i]);
+    }
+    // tokens i .. i + AT_ONCE - 1 (rows begin at any element: the reads are as aligned as those)
+    __device__ __forceinline__ void load(int i, float (&x)[AT_ONCE]) const {
+        typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
+        const words_t w = *reinterpret_cast<const words_t *>(p + i);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if constexpr (BF16) x[k] = counted(__uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16));
+            else x[k] = counted(__uint_as_float(w[k]));
+        }
+    }
+    // ... none from `end` on
+    __device__ __forceinline__ void load(int i, int end, float (&x)[AT_ONCE]) const {
+        if (i + AT_ONCE <= end) return load(i, x);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) x[k] = 0.0f;
+        if (i < end) {
+#pragma unroll
+            for (int k = 0; k < AT_ONCE - 1; ++k)
+                if (i + k < end) x[k] = (*this)[i + k];
+        }
     }
 };
 
@@ -43,173 +71,267 @@ template <bool BF16>
 __device__ __forceinline__ Row<BF16> draft_row(const VerifyCall &c, int s, int i) {
     return Row<BF16>::of(c.draft, s * c.draft_seq + i * c.draft_pos);
 }
-__device__ __forceinline__ int draft_count(const VerifyCall &c, int s) {
-    return c.draft_lens != nullptr ? min(max(c.draft_lens[s], 0), c.n_draft) : c.n_draft;
-}
 
-// Drafts of sequence s that stand; every wavefront finds them for itself, a draft per lane.
+// The drafts of sequence s, those that stand, and the one that fell.  Every wavefront looks for itself, a draft per lane: a read of what was drafted
+// and one of the probabilities that it goes by.
+struct Drafts {
+    int n, a, fell;
+};
 template <bool BF16>
-__device__ __forceinline__ int standing(const VerifyCall &c, int s, int n) {
+__device__ __forceinline__ Drafts standing(const VerifyCall &c, int s) {
     const int lane = threadIdx.x % kLanes;
-    for (int i0 = 0; i0 < n; i0 += kLanes) {
+    Drafts d{0, 0, -1};
+    for (int i0 = 0; i0 == 0 || i0 < d.n; i0 += kLanes) {
         const int i = i0 + lane;
-        bool stands = true;
-        if (i < n) {
-            const int x = c.tokens[static_cast<int64_t>(s) * c.n_draft + i];
-            const double u = uniform(c.uniforms[static_cast<int64_t>(s) * (c.n_draft + 1) + i]);
-            const bool is = x >= 0 && x < c.vocab;
-            const float p = is ? target_row<BF16>(c, s, i)[x] : 0.0f;
-            const float q = c.draft == nullptr ? 1.0f : (is ? draft_row<BF16>(c, s, i)[x] : 0.0f);
-            stands = u * q < p;       // (a product of two 24-bit numbers is exact in 64 bits)
+        int x = -1;
+        float u = 0.0f;
+        if (i < c.n_draft) {
+            x = c.tokens[static_cast<int64_t>(s) * c.n_draft + i];
+            u = c.uniforms[static_cast<int64_t>(s) * (c.n_draft + 1) + i];
         }
-        const uint64_t fallen = __ballot(!stands);
-        if (fallen != 0) return i0 + __ffsll(static_cast<unsigned long long>(fallen)) - 1;
+        if (i0 == 0) d.n = c.draft_lens != nullptr ? min(max(c.draft_lens[s], 0), c.n_draft) : c.n_draft;
+        const bool is = i < d.n && x >= 0 && x < c.vocab;
+        const float p = is ? target_row<BF16>(c, s, i)[x] : 0.0f;
+        const float q = c.draft == nullptr ? 1.0f : (is ? draft_row<BF16>(c, s, i)[x] : 0.0f);
+        const unsigned long long fallen = __ballot(i < d.n && !(uniform(u) * q < p));     // (a product of two 24-bit numbers is exact in 64 bits)
+        if (fallen != 0) {
+            const int at = __ffsll(fallen) - 1;
+            d.a = i0 + at;
+            d.fell = __builtin_amdgcn_readlane(x, at);
+            return d;
+        }
     }
-    return n;
+    d.a = d.n;
+    return d;
 }
 
-// What the token after the drafts is drawn from.
-template <bool BF16>
+constexpr int kRound = 1024;     // tokens that a wavefront has in registers
+
+// Of the lanes that have something the first that is past the goal, without one the last; -1: none has.
+__device__ __forceinline__ int first_past(bool some, bool past) {
+    const unsigned long long has = __ballot(some), hits = __ballot(some && past);
+    return hits != 0 ? __ffsll(hits) - 1 : (has != 0 ? 63 - __clzll(static_cast<long long>(has)) : -1);
+}
+
+// What the token after the drafts is drawn from: p less q (LESS: a draft of q fell), or p, without the token that fell if it had no
+// probabilities.
+template <bool BF16, bool LESS>
 struct Weights {
+    static constexpr int AT_ONCE = Row<BF16>::AT_ONCE;
     Row<BF16> p, q;
-    bool less;           // q is subtracted
-    int without;         // a token without weight (a draft that fell and has no probabilities), -1: none
-    __device__ __forceinline__ static Weights of(const VerifyCall &c, int s, int a, int n) {
-        Weights w;
-        w.p = target_row<BF16>(c, s, a);
-        w.less = a < n && c.draft != nullptr;
-        w.q = w.less ? draft_row<BF16>(c, s, a) : w.p;
-        w.without = a < n && c.draft == nullptr ? c.tokens[static_cast<int64_t>(s) * c.n_draft + a] : -1;
-        return w;
+    int vocab;
+    int without;         // that token, -1: none
+    __device__ __forceinline__ static Weights of(const VerifyCall &c, int s, const Drafts &d) {
+        return Weights{target_row<BF16>(c, s, d.a), LESS ? draft_row<BF16>(c, s, d.a) : Row<BF16>{}, c.vocab, c.draft == nullptr ? d.fell : -1};
     }
-    // of token v: p(v), and what is left of it
-    __device__ __forceinline__ double2 at(int v) const {
-        const double p = this->p[v];
-        return make_double2(p, v == without ? 0.0 : (less ? fmax(p - static_cast<double>(q[v]), 0.0) : p));
+    __device__ __forceinline__ static double rest(float x, float y) {
+        return LESS ? fmax(static_cast<double>(x) - static_cast<double>(y), 0.0) : static_cast<double>(x);
+    }
+    // A round of tokens from `at` on, none from `end` on: those of this lane, in a run of their own (RUN; for the one that goes on to
+    // look for a token) or 16 bytes at a time side by side with the other lanes'.
+    template <bool RUN>
+    struct Round {
+        static constexpr int READS = kRound / kLanes / AT_ONCE;
+        float x[READS][AT_ONCE], y[READS][AT_ONCE];
+        float left_out = 0.0f;       // what `without` had
+        __device__ __forceinline__ static int offset(int i) { return i * AT_ONCE * (RUN ? 1 : kLanes); }
+        __device__ __forceinline__ Round(const Weights &w, int at, int end, int without) {
+            const int first = at + static_cast<int>(threadIdx.x % kLanes) * (RUN ? kRound / kLanes : AT_ONCE);
+            if (at + kRound <= end) {
+#pragma unroll
+                for (int i = 0; i < READS; ++i) w.p.load(first + offset(i), x[i]);
+                if constexpr (LESS) {
+#pragma unroll
+                    for (int i = 0; i < READS; ++i) w.q.load(first + offset(i), y[i]);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < READS; ++i) {
+                    w.p.load(first + offset(i), end, x[i]);
+                    if constexpr (LESS) w.q.load(first + offset(i), end, y[i]);
+                }
+            }
+            if constexpr (!LESS) {
+                if (without < at || without >= at + kRound) return;
+#pragma unroll
+                for (int i = 0; i < READS; ++i)
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k)
+                        if (first + offset(i) + k == without) {
+                            left_out = x[i][k];
+                            x[i][k] = 0.0f;
+                        }
+            }
+        }
+    };
+    // A lane's sums over its tokens of [first, end).
+    __device__ __forceinline__ RowSums sum(int first, int end) const {
+        RowSums sum{0.0, 0.0};
+        for (int at = first; at < end; at += kRound) {
+            const Round<false> r(*this, at, end, without);
+#pragma unroll
+            for (int i = 0; i < r.READS; ++i)
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    if constexpr (LESS) sum.whole += r.x[i][k];
+                    sum.rest += rest(r.x[i][k], r.y[i][k]);
+                }
+            if constexpr (!LESS) sum.whole += r.left_out;
+        }
+        if constexpr (!LESS) sum.whole += sum.rest;
+        return sum;
+    }
+    // The first token of [first, end) whose weight is positive and whose running sum, from `before` on, exceeds the goal; without one
+    // the last one with a positive weight (sums in another order may miss the goal by their last bits), -1 where there is none.  First the
+    // lane whose run of tokens it is, and then a lane per token of that run, which is little code: code that runs once costs its fetch.
+    __device__ __forceinline__ int find(int first, int end, double before, double goal, bool of_rest) const {
+        constexpr int RUN = kRound / kLanes;
+        const int left_out = of_rest ? without : -1;
+        int token = -1;
+        for (int at = first; at < end; at += kRound) {
+            double own = 0.0;
+            {
+                const Round<true> r(*this, at, end, left_out);
+#pragma unroll
+                for (int i = 0; i < r.READS; ++i)
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) own += of_rest ? rest(r.x[i][k], r.y[i][k]) : static_cast<double>(r.x[i][k]);
+            }
+            const double upto = wave_scan(own);
+            const int lane = first_past(own > 0.0, before + upto > goal);
+            if (lane >= 0) {
+                const int v = at + lane * RUN + static_cast<int>(threadIdx.x % kLanes);
+                const bool there = threadIdx.x % kLanes < RUN && v < end && v != left_out;
+                const float x = there ? p[v] : 0.0f, y = LESS && there ? q[v] : 0.0f;
+                const double weight = of_rest ? rest(x, y) : static_cast<double>(x);
+                token = at + lane * RUN + first_past(weight > 0.0, before + wave_lane(upto - own, lane) + wave_scan(weight) > goal);
+                if (before + wave_lane(upto, lane) > goal) break;
+            }
+            before += wave_last(upto);
+        }
+        return token;
     }
 };
 
-// Inclusive sums over a wavefront's lanes, 64 bits.
-__device__ __forceinline__ double wave_scan(double x, int lane) {
+// The piece in which the running sum exceeds the goal, as Weights::find has it, and the sum before it, in the same way: sums[i], i < pieces,
+// kLanePieces of them a lane.
+constexpr int kLanePieces = kMostPieces / kLanes;
+struct Found {
+    int piece;
+    bool of_rest;
+    double before, goal;
+};
+__device__ __forceinline__ Found find_piece(const RowSums *sums, int pieces, float u) {
+    const int lane = threadIdx.x % kLanes;
+    RowSums sum{0.0, 0.0};
 #pragma unroll
-    for (int m = 1; m < kLanes; m *= 2) {
-        const double other = __shfl_up(x, m, kLanes);
-        x += lane >= m ? other : 0.0;
+    for (int i = 0; i < kLanePieces; ++i) {
+        const int at = lane * kLanePieces + i;
+        const RowSums piece = sums[min(at, pieces - 1)];
+        sum.whole += at < pieces ? piece.whole : 0.0;
+        sum.rest += at < pieces ? piece.rest : 0.0;
     }
-    return x;
-}
-// ... over a workgroup's threads; everybody's sum.  (all threads call this; one order of sums, whatever runs beside it)
-__device__ __forceinline__ double block_scan(double x, double *room, double *total) {
-    const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
-    const double upto = wave_scan(x, lane);
-    __syncthreads();
-    if (lane == kLanes - 1) room[wave] = upto;
-    __syncthreads();
-    double before = 0.0, all = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        before += w < wave ? room[w] : 0.0;
-        all += room[w];
-    }
-    *total = all;
-    return before + upto;
+    const double whole = wave_scan(sum.whole), rest = wave_scan(sum.rest);
+    Found f;
+    f.of_rest = wave_last(rest) > 0.0;     // (nothing left of a row, whose drafts were as likely as they were to be: all of it counts)
+    f.goal = uniform(u) * wave_last(f.of_rest ? rest : whole);
+    const double own = f.of_rest ? sum.rest : sum.whole, upto = f.of_rest ? rest : whole;
+    const int first = first_past(own > 0.0, upto > f.goal), at = max(first, 0) * kLanePieces + lane;
+    const RowSums mine = sums[min(at, pieces - 1)];
+    const double piece = lane < kLanePieces && at < pieces ? (f.of_rest ? mine.rest : mine.whole) : 0.0;
+    const double run = wave_lane(upto - own, max(first, 0)) + wave_scan(piece);
+    const int nth = first_past(piece > 0.0, run > f.goal);
+    f.piece = first < 0 ? -1 : first * kLanePieces + nth;
+    f.before = wave_lane(run - piece, max(nth, 0));
+    return f;
 }
 
-// A piece's two sums.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyCall c) {
-    __shared__ double room[kWaves];
-    const int s = blockIdx.y, n = draft_count(c, s), a = standing<BF16>(c, s, n);
-    const Weights<BF16> w = Weights<BF16>::of(c, s, a, n);
-    const int first = blockIdx.x * c.piece, last = min(first + c.piece, c.vocab);
-    double2 sum = make_double2(0.0, 0.0), total;
-    for (int v = first + threadIdx.x; v < last; v += kThreads) {
-        const double2 x = w.at(v);
-        sum.x += x.x;
-        sum.y += x.y;
-    }
-    block_scan(sum.x, room, &total.x);
-    block_scan(sum.y, room, &total.y);
-    if (threadIdx.x == 0) {
-        c.sums[static_cast<int64_t>(s) * c.pieces + blockIdx.x] = RowSums{total.x, total.y};
-        if (blockIdx.x == 0) c.accepted[s] = a;
-    }
-}
-
-// The token, and what the call says of the sequence.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void verify_pick_kernel(VerifyCall c) {
-    static_assert(kMostPieces <= kThreads, "a piece per thread");
-    __shared__ double room[kWaves], upto;
-    __shared__ int hit, last;
-    const int s = blockIdx.x, tid = threadIdx.x, n = draft_count(c, s), a = c.accepted[s];
-    const Weights<BF16> w = Weights<BF16>::of(c, s, a, n);
-    const RowSums mine = tid < c.pieces ? c.sums[static_cast<int64_t>(s) * c.pieces + tid] : RowSums{0.0, 0.0};
-    double2 total;
-    block_scan(mine.whole, room, &total.x);
-    block_scan(mine.rest, room, &total.y);
-    const bool rest = total.y > 0.0;         // (nothing left of a row, whose drafts were as likely as they were to be: all of it counts)
-    const double goal = uniform(c.uniforms[static_cast<int64_t>(s) * (c.n_draft + 1) + c.n_draft]) * (rest ? total.y : total.x);
-
-    // The first of the threads' values that is positive and whose running sum, from `before` on, exceeds the goal; without one the last
-    // positive one (sums in another order may miss the goal by their last bits); -1 where none is positive.  `upto`: the sum before it.
-    auto find = [&](double own, double before) {
-        double all;
-        const double run = before + block_scan(own, room, &all);
-        if (tid == 0) {
-            hit = kThreads;
-            last = -1;
-        }
-        __syncthreads();
-        if (own > 0.0) {
-            if (run > goal) atomicMin(&hit, tid);
-            atomicMax(&last, tid);
-        }
-        __syncthreads();
-        const int at = hit < kThreads ? hit : last;
-        if (tid == at) upto = run - own;
-        __syncthreads();
-        return at;
-    };
-    const int piece = find(rest ? mine.rest : mine.whole, 0.0);
-    int token = -1;
-    if (piece >= 0) {
-        const double before = upto;
-        const int each = c.piece / kThreads, first = piece * c.piece + tid * each, end = min(first + each, c.vocab);
-        double own = 0.0;
-        for (int v = first; v < end; ++v) {
-            const double2 x = w.at(v);
-            own += rest ? x.y : x.x;
-        }
-        if (find(own, before) == tid) {
-            double run = upto;
-            for (int v = first; v < end; ++v) {
-                const double2 both = w.at(v);
-                const double x = rest ? both.y : both.x;
-                if (x <= 0.0) continue;
-                token = v;
-                run += x;
-                if (run > goal) break;
-            }
-            last = token;
-        }
-        __syncthreads();
-        token = last;
-    }
-    for (int i = tid; i <= c.n_draft; i += kThreads)
+__device__ __forceinline__ void answer(const VerifyCall &c, int s, int a, int token) {
+    for (int i = threadIdx.x % kLanes; i <= c.n_draft; i += kLanes)
         c.tokens_out[static_cast<int64_t>(s) * (c.n_draft + 1) + i] = i < a ? c.tokens[static_cast<int64_t>(s) * c.n_draft + i] : (i == a ? token : -1);
+    if (threadIdx.x % kLanes == 0) c.accepted[s] = a;
+}
+__device__ __forceinline__ float last_uniform(const VerifyCall &c, int s) {
+    return c.uniforms[static_cast<int64_t>(s) * (c.n_draft + 1) + c.n_draft];
+}
+
+// f(weights) by the kind that the drafts leave.
+template <bool BF16, class F>
+__device__ __forceinline__ void with_weights(const VerifyCall &c, int s, const Drafts &d, F f) {
+    if (d.a < d.n && c.draft != nullptr) f(Weights<BF16, true>::of(c, s, d));
+    else f(Weights<BF16, false>::of(c, s, d));
+}
+
+// A workgroup per sequence; its wavefronts take the pieces in turns.
+constexpr int kRowWaves = 16;
+template <bool BF16>
+__global__ __launch_bounds__(kRowWaves * kLanes) void verify_row_kernel(VerifyCall c) {
+    __shared__ RowSums sums[kMostPieces];
+    const int s = blockIdx.x, lane = threadIdx.x % kLanes, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const float u = last_uniform(c, s);
+    const Drafts d = standing<BF16>(c, s);
+    with_weights<BF16>(c, s, d, [&](const auto &w) {
+        for (int i = wave; i < c.pieces; i += kRowWaves) {
+            const RowSums sum = w.sum(i * c.piece, min((i + 1) * c.piece, c.vocab));
+            const double whole = wave_scan(sum.whole), rest = wave_scan(sum.rest);
+            if (lane == kLanes - 1) sums[i] = RowSums{whole, rest};
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        const Found f = find_piece(sums, c.pieces, u);
+        const int first = f.piece * c.piece;
+        answer(c, s, d.a, f.piece < 0 ? -1 : w.find(first, min(first + c.piece, c.vocab), f.before, f.goal, f.of_rest));
+    });
+}
+
+// A wavefront per piece ...
+template <bool BF16>
+__global__ __launch_bounds__(kLanes) void verify_sums_kernel(VerifyCall c) {
+    const int s = blockIdx.y;
+    const Drafts d = standing<BF16>(c, s);
+    with_weights<BF16>(c, s, d, [&](const auto &w) {
+        const int first = blockIdx.x * c.piece;
+        const RowSums sum = w.sum(first, min(first + c.piece, c.vocab));
+        const double whole = wave_scan(sum.whole), rest = wave_scan(sum.rest);
+        if (threadIdx.x == kLanes - 1) c.sums[static_cast<int64_t>(s) * c.pieces + blockIdx.x] = RowSums{whole, rest};
+    });
+}
+
+// ... and one for the token.
+template <bool BF16>
+__global__ __launch_bounds__(kLanes) void verify_pick_kernel(VerifyCall c) {
+    const int s = blockIdx.x;
+    const float u = last_uniform(c, s);
+    const Drafts d = standing<BF16>(c, s);
+    with_weights<BF16>(c, s, d, [&](const auto &w) {
+        const Found f = find_piece(c.sums + static_cast<int64_t>(s) * c.pieces, c.pieces, u);
+        const int first = f.piece * c.piece;
+        answer(c, s, d.a, f.piece < 0 ? -1 : w.find(first, min(first + c.piece, c.vocab), f.before, f.goal, f.of_rest));
+    });
 }
 
 }  // namespace
 
-int launch_verify(const VerifyCall &c, void *stream) {
+int launch_verify(VerifyCall c, void *stream) {
     const hipStream_t on = static_cast<hipStream_t>(stream);
-    auto go = [&](auto sums, auto pick) {
-        hipLaunchKernelGGL(sums, dim3(c.pieces, c.n_seq), dim3(kThreads), 0, on, c);
-        hipLaunchKernelGGL(pick, dim3(c.n_seq), dim3(kThreads), 0, on, c);
-        return static_cast<int>(hipGetLastError());
-    };
-    return c.is_bf16 ? go(verify_sums_kernel<true>, verify_pick_kernel<true>) : go(verify_sums_kernel<false>, verify_pick_kernel<false>);
+    c.piece = (c.vocab / (kMostPieces * kRound) + 1) * kRound;
+    c.pieces = (c.vocab + c.piece - 1) / c.piece;
+    // Rows of up to 64 pieces in one launch, the others in two (us a call in a captured graph, fp32, one launch / two: 1 sequence x 8000 tokens 5.4 /
+    // 6.9, 1 x 32000 6.8 / 6.7, 64 x 32000 9.6 / 9.5, 512 x 32000 21 / 24, 8 x 50257 9.6 / 7.2, 1 x 64000 8.1 / 6.5, 1 x 128256 13.5 / 6.6,
+    // 64 x 128256 20 / 15, 256 x 128256 39 / 34; a launch costs its caller 4 us).
+    if (c.pieces <= 64) {
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(c.n_seq), dim3(kRowWaves * kLanes), 0, on, c); };
+        if (c.is_bf16) go(verify_row_kernel<true>);
+        else go(verify_row_kernel<false>);
+    } else {
+        auto go = [&](auto sums, auto pick) {
+            hipLaunchKernelGGL(sums, dim3(c.pieces, c.n_seq), dim3(kLanes), 0, on, c);
+            hipLaunchKernelGGL(pick, dim3(c.n_seq), dim3(kLanes), 0, on, c);
+        };
+        if (c.is_bf16) go(verify_sums_kernel<true>, verify_pick_kernel<true>);
+        else go(verify_sums_kernel<false>, verify_pick_kernel<false>);
+    }
+    return static_cast<int>(hipGetLastError());
 }
 
 }  // namespace octopus

@@ -53,9 +53,6 @@ int octopus_verify_drafts(const void *target, int32_t dtype, int64_t target_stri
     c.n_draft = n_draft;
     c.vocab = vocab;
     c.is_bf16 = dtype == OCTOPUS_DTYPE_BF16;
-    // pieces of whole multiples of 256 tokens, 1024 at least, and no more of them than have a thread each in the second launch
-    c.piece = std::max(1024, (vocab / kMostPieces + 256) / 256 * 256);
-    c.pieces = (vocab + c.piece - 1) / c.piece;
     return launch_verify(c, stream) == 0 ? OCTOPUS_OK : OCTOPUS_EHIP;
 }
 
