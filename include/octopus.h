@@ -554,12 +554,12 @@ int octopus_append_paged(const octopus_codebooks_t *cb,
  * (text has the same one on all of them).  Pair i goes by the axis that the caller's map gives it, whatever the map: a run of pairs an
  * axis, or the axes in turns.
  *   rope         host, not NULL.  (cos, sin) = table[p][i] with p the token's position on axis axis[i]; table, n_pos, dim and interleaved as
- *                in octopus_rope_t, positions outside [0, n_pos) read as the nearest inside.
+ *                in octopus_rope_t, positions outside [0, n_pos) read as the nearest inside; the table is at most 4 GiB, n_pos at most 2^24.
  *                pos: device int32, 4-byte aligned; axis k of new token t of sequence s at pos[s*stride_seq + t*stride_tok + k*stride_axis],
- *                strides in elements, >= 0 (0: the same for all).  Tokens from new_lens[s] on are not looked at.
+ *                strides in elements, >= 0 (0: the same for all), stride_tok below 2^31.  Tokens from new_lens[s] on are not looked at.
  *                axis: host [dim / 2] bytes, each below n_axes (1 .. OCTOPUS_MAX_AXES); read before the call returns.
  * With one axis, or the same position on all of them, every byte is that of octopus_append_paged.  Other arguments, launches and errors as there; EINVAL
- * also for rope NULL, pos or axis NULL, an axis past the last one, a negative stride. */
+ * also for rope NULL, pos or axis NULL, an axis past the last one, a stride or a table out of these ranges. */
 #define OCTOPUS_MAX_AXES 4
 typedef struct octopus_rope_axes {
     const float *table;

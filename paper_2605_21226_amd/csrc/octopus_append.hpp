@@ -6,7 +6,10 @@
 // pairs being channels i and i + dim / 2, or 2 i and 2 i + 1, i < dim / 2; channels from dim on stay.  It is applied in fp32 to the
 // key that the encoder takes: what octopus_encode_paged computes of rotated keys, without their rounding to bf16 in between.
 // A token of an image or a video has a position on each of several axes (frame, row, column), and pair i goes by the one that the
-// caller's map gives it: (cos, sin) = table[p_axis(i)][i].  Those kernels (append_*_axes_kernel) differ in nothing else.
+// caller's map gives it: (cos, sin) = table[p_axis(i)][i].  Those kernels (append_*_axes_kernel) differ in nothing else.  A pair's entry is
+// read by itself there, whatever the map, twice as many reads as of one position's row: 15840 patches take 111 us where tokens in a row take
+// 96 (94 if the reads were as wide and no positions had to be read), 64 single tokens 8.0 instead of 7.4.  Wide reads for maps that allow
+// them, beside these by a branch, cost more than they saved (113), by threads too (114).
 //
 // What bounds it: memory, for long prompts -- queries, keys and values come and go once, the records are a quarter of the keys -- and
 // latency for a few tokens.  Measured at d = 128, 3 bits, 32 query and 8 KV heads, bf16: 15877 tokens, 366 MB, in 97 us, 3.8 TB/s
@@ -44,6 +47,13 @@ __device__ __forceinline__ void store_eight(void *base, int64_t at, int is_bf16,
     }
 }
 
+// The table's rows of a token's positions on its axes, in bytes from its start.  (Four numbers, and handed on by value: the compiler
+// puts into LDS what elements are chosen from by address, and reads the dispatch packet, in host memory, to find it there: 12 us.)
+struct AxisRows {
+    uint32_t r0, r1, r2, r3;
+};
+static_assert(kMaxAxes == 4, "");
+
 // A thread's eight channels' (cos, sin) of a position, and the rotation of its share of a row.  Rows lie LPR lanes side by side, so
 // that a channel's partner half a rotation away is half a rotation / 8 lanes away.
 template <int LPR>
@@ -68,29 +78,32 @@ struct RowRotation {
             cs[j + 1] = make_float2(two.z, two.w);
         }
     }
-    // ... of a token's positions on several axes, at p[0], p[stride], ...
-    template <int WORDS>
-    __device__ __forceinline__ void load(const RopeCall &r, const AxesCall &x, const int32_t *p, int col) {
+    // The first of a thread's pairs, and the axes of its eight (two bits each).
+    __device__ __forceinline__ static int first_pair(const RopeCall &r, int col) {
+        return r.interleaved != 0 ? col / 2 : (col >= r.dim / 2 ? col - r.dim / 2 : col);
+    }
+    __device__ __forceinline__ static uint32_t axes_of(const RopeCall &r, const AxesCall &x, int col) {
+        const int first = first_pair(r, col);
+        uint32_t axes = x.axis_of[0];            // 16 pairs a word
+#pragma unroll
+        for (int w = 1; w < LPR / 4; ++w) axes = first / 16 == w ? x.axis_of[w] : axes;
+        return axes >> (2 * (first % 16));
+    }
+    // ... of a token's positions on several axes, of which the table's rows are
+    __device__ __forceinline__ void load(const RopeCall &r, uint32_t axes, AxisRows rows, int col) {
         half = col < r.dim ? r.dim / 2 : 0;
         pairs = r.interleaved != 0;
         upper = col >= half;
         if (half == 0) return;
-        const int first = pairs ? col / 2 : (upper ? col - half : col);
-        uint32_t axes = x.axis_of[0];            // two bits a pair, 16 pairs a word
-#pragma unroll
-        for (int w = 1; w < WORDS; ++w) axes = first / 16 == w ? x.axis_of[w] : axes;
-        axes >>= 2 * (first % 16);
-        const float2 *row[kMaxAxes];
-#pragma unroll
-        for (int k = 0; k < kMaxAxes; ++k) {     // (axes past the last: the last again)
-            const int64_t pos = p[min(k, x.n_axes - 1) * x.stride_axis];
-            row[k] = reinterpret_cast<const float2 *>(r.table) + min(max(pos, static_cast<int64_t>(0)), r.n_pos - 1) * half + first;
-        }
+        const int first = first_pair(r, col);
+        const uint32_t r0 = rows.r0 + 8 * first, r1 = rows.r1 + 8 * first, r2 = rows.r2 + 8 * first, r3 = rows.r3 + 8 * first;
+        auto bit = [axes](int i) { return static_cast<uint32_t>(static_cast<int32_t>(axes << (31 - i)) >> 31); };      // all ones or none
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             if (j >= 4 && pairs) break;
-            const uint32_t k = (axes >> (2 * j)) & 3u;
-            cs[j] = (k & 2u ? (k & 1u ? row[3] : row[2]) : (k & 1u ? row[1] : row[0]))[j];
+            const uint32_t odd = bit(2 * j), upper_two = bit(2 * j + 1);      // (selected bit by bit, see AxisRows)
+            const uint32_t lo = (r1 & odd) | (r0 & ~odd), hi = (r3 & odd) | (r2 & ~odd), at = (hi & upper_two) | (lo & ~upper_two);
+            cs[j] = *reinterpret_cast<const float2 *>(reinterpret_cast<const char *>(r.table) + at + 8 * j);
         }
     }
     // (all lanes of a row call this: the partners' channels come from other lanes.  One rounding order, whatever the caller: a key has
@@ -128,31 +141,47 @@ __device__ __forceinline__ int64_t append_page(const AppendCall &a, int seq, int
     return min(max(a.pt.table[static_cast<int64_t>(seq) * a.pt.stride + tile], 0), a.pt.n_pages - 1);
 }
 
-// Where a token's rotation comes from: one position, or one on each axis.
+// Where a token's rotation comes from: one position, or one on each axis.  `at` reads the positions of a slot, `load` the (cos, sin) there:
+// what else a caller reads goes in between, since the one waits for the other.
 struct OneAxis {
+    static constexpr bool LATE = false;     // nothing is waited for
     struct Sequence {
+        using Place = int64_t;
         int64_t pos0;      // the position of slot 0, if it were there
+        __device__ __forceinline__ Place at(const AppendCall &, int64_t slot) const { return pos0 + slot; }
         template <int LPR>
-        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, int64_t slot, int col) const { rot.load(a.rope, pos0 + slot, col); }
+        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, const Place &place, int col) const { rot.load(a.rope, place, col); }
     };
-    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start) const { return {append_position(a, seq, start) - start}; }
+    template <int LPR>
+    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start, int) const { return {append_position(a, seq, start) - start}; }
 };
 struct ManyAxes {
+    static constexpr bool LATE = true;
     AxesCall x;
     struct Sequence {
+        using Place = AxisRows;
         const AxesCall &x;
         const int32_t *pos;
         int64_t start;
-        int count;         // tokens that have positions, 1 at least
-        template <int LPR>
-        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, int64_t slot, int col) const {
-            // (a tile's slots in front of the first token and behind the last one ask as well, and get the nearest token's)
-            const int64_t tok = min(max(slot - start, static_cast<int64_t>(0)), static_cast<int64_t>(count) - 1);
-            rot.template load<LPR / 4>(a.rope, x, pos + tok * x.stride_tok, col);
+        int last;          // token that has positions
+        uint32_t axes;     // of the thread's pairs
+        __device__ __forceinline__ Place at(const AppendCall &a, int64_t slot) const {
+            // (a tile's slots in front of the first token and behind the last one ask as well, and get the nearest token's; an axis past the last
+            // reads the first one's position: four reads that wait for nothing but each other are one wait)
+            const uint32_t tok = min(max(static_cast<int32_t>(slot - start), 0), last);
+            const int32_t *p = pos + static_cast<uint64_t>(tok) * static_cast<uint32_t>(x.stride_tok);
+            const int32_t p0 = p[0], p1 = p[x.axis_at[0]], p2 = p[x.axis_at[1]], p3 = p[x.axis_at[2]];
+            auto row = [&](int32_t at) { return static_cast<uint32_t>(__umul24(min(max(at, 0), x.last_pos), 4 * a.rope.dim)); };
+            return Place{row(p0), row(p1), row(p2), row(p3)};
         }
+        template <int LPR>
+        __device__ __forceinline__ void load(RowRotation<LPR> &rot, const AppendCall &a, Place place, int col) const { rot.load(a.rope, axes, place, col); }
     };
-    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start) const {
-        return {x, x.pos + seq * x.stride_seq, start, append_count(a, seq)};
+    template <int LPR>
+    __device__ __forceinline__ Sequence of(const AppendCall &a, int seq, int64_t start, int col) const {
+        uint32_t axes = RowRotation<LPR>::axes_of(a.rope, x, col);
+        asm("" : "+v"(axes));      // (kept, and not read again for every token)
+        return {x, x.pos + seq * x.stride_seq, start, append_count(a, seq) - 1, axes};
     }
 };
 
@@ -173,8 +202,10 @@ __device__ __forceinline__ void append_token(const AppendCall &a, const Turn &tu
     // (a token past what the table reaches is written nowhere; its queries are rotated all the same)
     const bool reached = slot < static_cast<int64_t>(a.pt.stride) * kWave;
     const int64_t tile = reached ? (append_page(a, seq, slot / kWave) * a.n_kv_heads + kvh) : 0;
+    const auto turns = turn.template of<LPR>(a, seq, start, col);
+    const auto place = turns.at(a, slot);
     RowRotation<LPR> rot;
-    turn.of(a, seq, start).load(rot, a, slot, col);
+    if constexpr (!Turn::LATE) turns.load(rot, a, place, col);
 
     const int hpk = a.q != nullptr ? a.n_q_heads / a.n_kv_heads : 0;
     float key[8];
@@ -187,6 +218,8 @@ __device__ __forceinline__ void append_token(const AppendCall &a, const Turn &tu
         if (row == 0) load_eight(a.k, seq * a.k_seq + tok * a.k_tok + kvh * a.k_head + col, a.kv_is_bf16, x);
         else if (row == 1 && a.v_pool != nullptr) load_eight(a.v, seq * a.v_seq + tok * a.v_tok + kvh * a.v_head + col, a.kv_is_bf16, x);
         else if (row > 1 && row < 2 + hpk) load_eight(a.q, seq * a.q_seq + tok * a.q_tok + (kvh * hpk + row - 2) * a.q_head + col, a.q_is_bf16, x);
+        if constexpr (Turn::LATE)
+            if (r0 == 0) turns.load(rot, a, place, col);
         if (row == 1 && a.v_pool != nullptr && reached) store_eight(a.v_pool, (tile * kWave + slot % kWave) * D + col, 1, x);
         rot.apply(x, lane);
         if (row > 1 && row < 2 + hpk) store_eight(a.q_out, qrow * D + col, a.q_out_is_bf16, x);
@@ -316,8 +349,9 @@ __device__ __forceinline__ void append_tile(const AppendCall &a, const Turn &tur
             }
         }
         if (last > values) {
+            const auto turns = turn.template of<LPR>(a, seq, start, col);
             RowRotation<LPR> rot;
-            turn.of(a, seq, start).load(rot, a, slot, col);
+            turns.load(rot, a, turns.at(a, slot), col);
             const int64_t out = (static_cast<int64_t>(seq) * a.n_new + tok) * a.n_q_heads;
             for (int h0 = max(first - values, 0); h0 < last - values; h0 += kAhead) {
                 float x[kAhead][8];
@@ -341,7 +375,7 @@ __device__ __forceinline__ void append_tile(const AppendCall &a, const Turn &tur
     const int64_t first_tile = start / kWave + static_cast<int64_t>(run) * tiles_per_group;
     if (max(first_tile * kWave, start) >= tok_end) return;
     const int64_t head_base = seq * a.k_seq + kvh * a.k_head + col;
-    const auto turns = turn.of(a, seq, start);
+    auto turns = turn.template of<LPR>(a, seq, start, col);
     const uint32_t sbits = a.signs[kvh * LPR + col / 8];
 
     // a tile's key rows: eight coordinates per thread and pass, rotated; rows outside [start, tok_end) are zeros
@@ -391,7 +425,7 @@ __device__ __forceinline__ void append_tile(const AppendCall &a, const Turn &tur
             const int key = pass * RPP + tid / LPR;
             float (&x)[8] = rows[pass];
             RowRotation<LPR> rot;
-            turns.load(rot, a, tile * kWave + key, col);
+            turns.load(rot, a, turns.at(a, tile * kWave + key), col);
             rot.apply(x, lane);
             float ss = 0.0f;
 #pragma unroll

@@ -189,14 +189,15 @@ struct RopeCall {
     const int32_t *pos;
     int32_t dim, interleaved;
 };
-// ... by positions of several axes: axis k of token t of sequence s at pos[s stride_seq + t stride_tok + k stride_axis], pair i by axis
-// (axis_of[i / 16] >> 2 (i % 16)) & 3 (RopeCall::pos is not looked at).
+// ... by positions of several axes: that of token t of sequence s on the first axis at pos[s stride_seq + t stride_tok], on the others
+// axis_at[] behind it (0 for axes that are not there), pair i by axis (axis_of[i / 16] >> 2 (i % 16)) & 3 (RopeCall::pos is not looked at).
 constexpr int kMaxAxes = OCTOPUS_MAX_AXES;
 struct AxesCall {
     const int32_t *pos;
-    int64_t stride_seq, stride_tok, stride_axis;
+    int64_t stride_seq, axis_at[kMaxAxes - 1];
+    int32_t stride_tok;
     uint32_t axis_of[8];
-    int32_t n_axes;
+    int32_t last_pos;       // of the table that a position can name
 };
 // Appending to pages (octopus_append.hpp).  v_pool NULL: the values are quantised by a launch of their own; q NULL: no queries.
 struct AppendCall {

@@ -76,7 +76,10 @@ int append(const octopus_codebooks_t *cb, const void *k, int64_t k_stride_seq, i
     if (axes != nullptr) {
         if (axes->table == nullptr || !aligned(axes->table, 16) || axes->n_pos < 1 || axes->pos == nullptr || !aligned(axes->pos, 4)) return OCTOPUS_EINVAL;
         if (axes->dim < 16 || axes->dim > d || axes->dim % 16 != 0 || (axes->interleaved != 0 && axes->interleaved != 1)) return OCTOPUS_EINVAL;
-        if (axes->stride_seq < 0 || axes->stride_tok < 0 || axes->stride_axis < 0) return OCTOPUS_EINVAL;
+        // (the table is addressed by 32 bits of bytes, rows by a product of 24 bits each, a token's positions by one of 32)
+        if (axes->n_pos > (int64_t{1} << 32) / (4 * axes->dim) || axes->n_pos > (1 << 24)) return OCTOPUS_EINVAL;
+        if (axes->stride_seq < 0 || axes->stride_tok < 0 || axes->stride_tok > INT32_MAX || axes->stride_axis < 0 || axes->stride_axis > INT64_MAX / (8 * kMaxAxes))
+            return OCTOPUS_EINVAL;
         if (axes->n_axes < 1 || axes->n_axes > kMaxAxes || axes->axis == nullptr) return OCTOPUS_EINVAL;
         for (int i = 0; i < axes->dim / 2; ++i) {
             if (axes->axis[i] >= axes->n_axes) return OCTOPUS_EINVAL;
@@ -84,9 +87,9 @@ int append(const octopus_codebooks_t *cb, const void *k, int64_t k_stride_seq, i
         }
         many.pos = axes->pos;
         many.stride_seq = axes->stride_seq;
-        many.stride_tok = axes->stride_tok;
-        many.stride_axis = axes->stride_axis;
-        many.n_axes = axes->n_axes;
+        many.stride_tok = static_cast<int32_t>(axes->stride_tok);
+        for (int k = 1; k < axes->n_axes; ++k) many.axis_at[k - 1] = k * axes->stride_axis;
+        many.last_pos = static_cast<int32_t>(axes->n_pos - 1);
         a.rope = RopeCall{axes->table, axes->n_pos, nullptr, axes->dim, axes->interleaved};
         a.axes = &many;
     }
