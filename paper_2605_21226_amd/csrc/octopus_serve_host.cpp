@@ -74,7 +74,8 @@ int append(const octopus_codebooks_t *cb, const void *k, int64_t k_stride_seq, i
     }
     AxesCall many{};
     if (axes != nullptr) {
-        if (axes->table == nullptr || !aligned(axes->table, 16) || axes->n_pos < 1 || axes->pos == nullptr || !aligned(axes->pos, 4)) return OCTOPUS_EINVAL;
+        if (axes->table == nullptr || !aligned(axes->table, 16) || axes->n_pos < 1 || (n_new != 0 && axes->pos == nullptr) || !aligned(axes->pos, 4))
+            return OCTOPUS_EINVAL;
         if (axes->dim < 16 || axes->dim > d || axes->dim % 16 != 0 || (axes->interleaved != 0 && axes->interleaved != 1)) return OCTOPUS_EINVAL;
         // (the table is addressed by 32 bits of bytes, rows by a product of 24 bits each, a token's positions by one of 32)
         if (axes->n_pos > (int64_t{1} << 32) / (4 * axes->dim) || axes->n_pos > (1 << 24)) return OCTOPUS_EINVAL;

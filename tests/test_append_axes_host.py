@@ -25,14 +25,15 @@ def test_refusals(lib):  # noqa: F811
     refuses(lib.octopus_append_paged_axes, APPEND, good, [
         ({}, OK), ({"rope": None}, EINVAL),
         *[({"rope": rope(**k)}, EINVAL) for k in (
-            dict(table=None), dict(table=OFF8), dict(n_pos=0), dict(n_pos=-5), dict(n_pos=2 ** 23 + 1), dict(dim=16, n_pos=2 ** 24 + 1), dict(n_pos=2 ** 62), dict(pos=None), dict(pos=FAKE + 2), dict(dim=0), dict(dim=8),
+            dict(table=None), dict(table=OFF8), dict(n_pos=0), dict(n_pos=-5), dict(n_pos=2 ** 23 + 1), dict(dim=16, n_pos=2 ** 24 + 1), dict(n_pos=2 ** 62), dict(pos=FAKE + 2), dict(dim=0), dict(dim=8),
             dict(dim=24), dict(dim=144), dict(dim=-16), dict(interleaved=2), dict(interleaved=-1), dict(n_axes=0), dict(n_axes=-1), dict(n_axes=5), dict(n_axes=2),
             dict(axis=None), dict(axis=late), dict(stride_seq=-1), dict(stride_tok=-1), dict(stride_tok=2 ** 31), dict(stride_axis=-1))],
         # (pairs past dim / 2 have no axis: nothing there is looked at)
         *[({"rope": rope(**k)}, OK) for k in (dict(axis=late, dim=112), dict(axis=late, n_axes=4), dict(stride_seq=0, stride_tok=0, stride_axis=0),
-                                              dict(interleaved=1), dict(n_pos=2 ** 23), dict(dim=16, n_pos=2 ** 24), dict(stride_tok=2 ** 31 - 1), dict(dim=16, axis=bytes(8), n_axes=1))],
+                                              dict(interleaved=1), dict(pos=None), dict(n_pos=2 ** 23), dict(dim=16, n_pos=2 ** 24), dict(stride_tok=2 ** 31 - 1), dict(dim=16, axis=bytes(8), n_axes=1))],
         *[({name: None}, EINVAL) for name in ("cb", "signs", "k_pool", "v_pool", "block_table", "q_out")],
         *[({name: n}, EINVAL) for name in ("n_seq", "n_kv", "n_pages", "max_pages", "n_qh") for n in (0, -1)],
+        ({"n_new": 1, "rope": rope(pos=None)}, EINVAL), ({"k": None, "v": None, "q": None, "rope": rope(pos=None)}, OK),     # (an empty tensor may have no address)
         ({"n_new": -1}, EINVAL), ({"n_qh": 30}, EINVAL), ({"kt": 4}, EINVAL), ({"kv_dtype": 2}, EUNSUPPORTED),
         ({"cb": ctypes.byref(broken)}, EINVAL), ({"cb": ctypes.byref(unbuilt)}, EUNSUPPORTED)])
 
