@@ -254,12 +254,12 @@ def _dtype_code(t):
     return code
 
 
-def _is_int32(t):
+def _int32_type():
     global _int32
     if _int32 is None:
         import torch
         _int32 = torch.int32
-    return t.dtype is _int32
+    return _int32
 
 
 def _stream_ptr(stream):
@@ -605,7 +605,7 @@ def octopus_append_paged_axes(cb, k, v, signs, k_pool, v_pool, n_pages, block_ta
     assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
     axis = rope_axis if type(rope_axis) is bytes else bytes(rope_axis)
     p_seq, p_new, n_axes = rope_pos.shape
-    assert len(axis) == pairs and p_seq == k.shape[0] and p_new == k.shape[1] and _is_int32(rope_pos)
+    assert len(axis) == pairs and p_seq == k.shape[0] and p_new == k.shape[1] and rope_pos.dtype is _int32_type()
     turn = ctypes.byref(RopeAxes(rope.data_ptr(), n_pos, rope_pos.data_ptr(), *rope_pos.stride(), axis, n_axes, 2 * pairs,
                                  1 if rope_interleaved else 0))
     _append("octopus_append_paged_axes", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
@@ -656,8 +656,9 @@ def octopus_pages_workspace(n_pages, n_seq, max_pages_per_seq):
 
 def _check_ints(*tensors):
     """That each (tensor or None, least number of elements) is contiguous int32 of at least as many."""
+    int32 = _int32_type()
     for t, least in tensors:
-        assert t is None or (_is_int32(t) and t.is_contiguous() and t.numel() >= least)
+        assert t is None or (t.dtype is int32 and t.is_contiguous() and t.numel() >= least)
 
 
 def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, source=None, keep_lens=None, stream=None):
