@@ -672,13 +672,14 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb,
  *                to octopus_pages_copy before anything is appended; no page is both a from and a to.
  *     workspace  device, 256-byte aligned, octopus_pages_workspace(...) bytes of the same shape (which does not shrink as a number grows);
  *                contents are scratch.
- *   One launch; three with a source.
+ *   One launch; three with a source and more than 1024 slots or 8192 table entries.
  *
  * octopus_pages_compact: moves the pages in use to the front of the pools: with n of them in use, the highest goes to the lowest free one, the next
  *   to the next, until they are 0 .. n - 1.
  *     page_map   device int32 [n_pages]: a page's new number (its own where it stays).
  *     moves      device int32 [2 + 2 (n_pages / 2)]: [0] pages to be copied, [1] n, then (from, to) pairs, highest page first.
- *   refs follow.  Every table has to follow by octopus_pages_rename, and every pool by octopus_pages_copy.  Three launches.
+ *   refs follow.  Every table has to follow by octopus_pages_rename, and every pool by octopus_pages_copy.  One launch up to 65536 pages,
+ *   else three.
  * octopus_pages_rename: entries below ceil(lens[r] / 64) of each row r (lens NULL: all) become page_map[entry]; a block table, or
  *   (n_rows 1, prefix_len) a prefix_table.
  *
@@ -739,7 +740,7 @@ int octopus_pages_copy(const octopus_pool_t *pools, int32_t n_pools, int32_t n_p
  *   workspace    device, 256-byte aligned, at least octopus_verify_workspace(...) bytes (which does not shrink as a number grows); scratch.
  * Probabilities that are no positive finite numbers count as 0.  Where no r(v) is positive though a draft fell, the token is drawn from p_a;
  * where no p_a(v) is either, it is -1.  n_draft 0 (draft and draft_tokens NULL): one token drawn from each sequence's p_0.
- * Two launches.  Outputs overlap no input.
+ * One launch up to a vocabulary of 65536, else two.  Outputs overlap no input.
  * Errors: EINVAL (NULL or misaligned pointers, negative strides, n_seq outside 1 .. 65535, n_draft outside 0 .. 2^20, vocab outside 1 .. 2^30),
  * EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */
 size_t octopus_verify_workspace(int32_t n_seq, int32_t n_draft, int32_t vocab);

@@ -114,8 +114,17 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
     __shared__ int room[2][kAssignThreads / kScanLanes];
     __shared__ int first_of[kAssignThreads], entry_of[kAssignThreads], fresh[kAssignThreads];
     __shared__ int flags[4];
+    // ONE: pages that several would write into, found by their number, with the writers' count and the first of them
+    constexpr int kTable = 2 * kAssignThreads;
+    __shared__ int page_at[ONE ? kTable : 1], writers_at[ONE ? kTable : 1], first_at[ONE ? kTable : 1];
     const int tid = threadIdx.x;
     if (tid < 4) flags[tid] = 0;
+    if constexpr (ONE)
+        for (int i = tid; i < kTable; i += kAssignThreads) {
+            page_at[i] = -1;
+            writers_at[i] = 0;
+            first_at[i] = INT32_MAX;
+        }
     __syncthreads();
     // whether it holds for any thread, in this round or one before (all threads call it; a barrier)
     auto any = [&](int which, bool it) {
@@ -127,10 +136,6 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
     };
     SlotPages mine{0, 0, -1, 0};         // ONE: the thread's slot
     auto slot = [&](int s) { return ONE ? mine : c.info[s]; };
-    auto set_copied = [&](int s) {
-        if constexpr (ONE) mine.copied = 1;
-        else c.info[s].copied = 1;
-    };
     __shared__ Slot slots[ROWS ? kAssignThreads : 1];
     __shared__ int page_in[ROWS ? kAssignThreads : 1], pages_stay[ROWS ? kAssignThreads : 1];
     int32_t row[kEntries];               // ROWS: what the thread's entries become, -1: nothing new
@@ -222,11 +227,26 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
     __syncthreads();
     uint32_t free = free_pages(c, tid * kPerThread);
     bool shared = false;
+    int holders = 0;                     // ONE: of the page that the thread's slot writes into
     for (int s = tid; s < c.n_seq; s += kAssignThreads) {
         const int page = page_of(s);
-        shared |= page >= 0 && load_count(&c.refs[page]) > 1;
+        if (page >= 0) holders = load_count(&c.refs[page]);
+        shared |= page >= 0 && holders > 1;
     }
-    if (any(1, shared)) {
+    if constexpr (ONE) {
+        if (any(1, shared)) {
+            int at = 0;
+            if (shared) {
+                at = static_cast<uint32_t>(my_page) * 2654435761u >> 21;          // (a half empty table: a free place is found)
+                static_assert(kTable == 1 << 11, "");
+                for (int other; (other = atomicCAS(&page_at[at], -1, my_page)) != -1 && other != my_page;) at = (at + 1) % kTable;
+                atomicAdd(&writers_at[at], 1);
+                atomicMin(&first_at[at], rank(tid, mine));
+            }
+            __syncthreads();
+            if (shared && (holders > writers_at[at] || first_at[at] != rank(tid, mine))) mine.copied = 1;
+        }
+    } else if (any(1, shared)) {
         for (int s = tid; s < c.n_seq; s += kAssignThreads) {
             const int page = page_of(s);
             if (page >= 0) {
@@ -245,7 +265,7 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
         __syncthreads();
         for (int s = tid; s < c.n_seq; s += kAssignThreads) {
             const int page = page_of(s);
-            if (page >= 0 && (load_count(&c.refs[page]) > load_count(&c.writers[page]) || load_count(&c.first[page]) != rank(s, slot(s)))) set_copied(s);
+            if (page >= 0 && (load_count(&c.refs[page]) > load_count(&c.writers[page]) || load_count(&c.first[page]) != rank(s, slot(s)))) c.info[s].copied = 1;
         }
     }
 
@@ -346,18 +366,29 @@ __device__ __forceinline__ uint32_t used_pages(const PagesCall &c, int64_t at) {
     const int64_t there = min(max(c.n_pages - at, static_cast<int64_t>(0)), static_cast<int64_t>(kPerThread));
     return ~free_pages(c, at) & ((1u << there) - 1u);
 }
-// Pages from `at` on, of which `used` are in use and `n` below them: their places in `moves`, and in the map those of the pages that stay.
+// Pages from `at` on, of which `used` are in use and `n` below them: their places in `moves`, and in the map those of the pages that stay
+// (the others' are written with their moves, later).
 __device__ __forceinline__ void pair_pages(const PagesCall &c, int64_t at, uint32_t used, int n, int n_used) {
-    for (int i = 0; i < kPerThread; ++i) {
-        const int id = static_cast<int>(at) + i;
-        if (id >= c.n_pages) break;
-        const bool is = (used >> i) & 1u;
-        if (is && id >= n_used) c.moves[2 + 2 * (n_used - 1 - n)] = id;
-        else c.page_map[id] = id;
-        if (!is && id < n_used) c.moves[3 + 2 * (id - n)] = id;
-        n += is ? 1 : 0;
-        if (id == n_used - 1) c.moves[0] = n_used - n;      // free pages below n_used
+    if (at >= c.n_pages) return;
+    const int first = static_cast<int>(at), there = min(c.n_pages - first, kPerThread);
+    if (there == kPerThread) {
+        typedef int32_t ids_t __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int i = 0; i < kPerThread; i += 4) *reinterpret_cast<ids_t *>(c.page_map + first + i) = ids_t{first + i, first + i + 1, first + i + 2, first + i + 3};
+    } else {
+        for (int i = 0; i < there; ++i) c.page_map[first + i] = first + i;
     }
+    const int below = min(max(n_used - first, 0), kPerThread);          // of these pages that lie below n_used
+    const uint32_t all = (1u << there) - 1u, low = (1u << below) - 1u;
+    for (uint32_t high = used & all & ~low; high != 0; high &= high - 1) {
+        const int i = __ffs(high) - 1;
+        c.moves[2 + 2 * (n_used - 1 - (n + static_cast<int>(__popc(used & ((1u << i) - 1u)))))] = first + i;
+    }
+    for (uint32_t free = ~used & all & low; free != 0; free &= free - 1) {
+        const int i = __ffs(free) - 1;
+        c.moves[3 + 2 * (first + i - (n + static_cast<int>(__popc(used & ((1u << i) - 1u)))))] = first + i;
+    }
+    if (first < n_used && n_used <= first + there) c.moves[0] = n_used - (n + static_cast<int>(__popc(used & low)));      // free pages below n_used
     if (at == 0) {
         c.moves[1] = n_used;
         if (n_used == 0) c.moves[0] = 0;
@@ -432,10 +463,10 @@ __global__ __launch_bounds__(kCountThreads) void pages_apply_kernel(PagesCall c)
 
 __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(PagesCall c) {
     const int s = blockIdx.y, j = blockIdx.x * kRowThreads + threadIdx.x;
-    const int n = c.lens != nullptr ? min(pages_of(min(max(c.lens[s], 0), c.max_pages * OCTOPUS_TILE)), c.max_pages) : c.max_pages;
-    if (j >= n) return;
+    if (j >= c.max_pages) return;
     const int64_t at = static_cast<int64_t>(s) * c.max_pages + j;
-    c.table[at] = c.page_map[page_id(c, c.table[at])];
+    const int page = page_id(c, c.table[at]);        // (asked for beside the length)
+    if (c.lens == nullptr || j < pages_of(min(max(c.lens[s], 0), c.max_pages * OCTOPUS_TILE))) c.table[at] = c.page_map[page];
 }
 
 // A pool's pages by blockIdx.y, pieces of 16 KB of the moved pages by blockIdx.x.  What is written streams past the caches, what is read
