@@ -654,11 +654,9 @@ def octopus_pages_workspace(n_pages, n_seq, max_pages_per_seq):
     return int(load().octopus_pages_workspace(int(n_pages), int(n_seq), int(max_pages_per_seq)))
 
 
-def _check_ints(*tensors):
-    """That each (tensor or None, least number of elements) is contiguous int32 of at least as many."""
-    int32 = _int32_type()
-    for t, least in tensors:
-        assert t is None or (t.dtype is int32 and t.is_contiguous() and t.numel() >= least)
+def _ints_ok(t, least):
+    """That a tensor (or None) is contiguous int32 of at least so many elements."""
+    return t is None or (t.dtype is (_int32 or _int32_type()) and t.is_contiguous() and t.numel() >= least)
 
 
 def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, source=None, keep_lens=None, stream=None):
@@ -666,7 +664,8 @@ def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, so
     [n_pages], block_table device int32 [n_seq, max_pages_per_seq], lens, new_lens, source and keep_lens device int32 [n_seq], moves
     device int32 of at least 2 + 2 n_seq, workspace device uint8 of octopus_pages_workspace(...)."""
     n_seq, max_pages = block_table.shape
-    _check_ints((refs, 1), (block_table, 1), (lens, n_seq), (new_lens, n_seq), (source, n_seq), (keep_lens, n_seq), (moves, 2 + 2 * n_seq))
+    assert _ints_ok(refs, 1) and _ints_ok(block_table, 1) and _ints_ok(lens, n_seq) and _ints_ok(new_lens, n_seq)
+    assert _ints_ok(source, n_seq) and _ints_ok(keep_lens, n_seq) and _ints_ok(moves, 2 + 2 * n_seq)
     code = load().octopus_pages_update(refs.data_ptr(), refs.numel(), block_table.data_ptr(), max_pages, lens.data_ptr(), n_seq, _ptr(source),
                                        _ptr(keep_lens), new_lens.data_ptr(), moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                        _stream_ptr(stream))
@@ -676,7 +675,7 @@ def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, so
 def octopus_pages_compact(refs, page_map, moves, workspace, stream=None):
     """The pages in use to the front: refs and page_map device int32 [n_pages], moves device int32 of at least 2 + 2 (n_pages // 2)."""
     n_pages = refs.numel()
-    _check_ints((refs, 1), (page_map, n_pages), (moves, 2 + 2 * (n_pages // 2)))
+    assert _ints_ok(refs, 1) and _ints_ok(page_map, n_pages) and _ints_ok(moves, 2 + 2 * (n_pages // 2))
     code = load().octopus_pages_compact(refs.data_ptr(), n_pages, page_map.data_ptr(), moves.data_ptr(), workspace.data_ptr(),
                                         workspace.nbytes, _stream_ptr(stream))
     _check(code, "octopus_pages_compact")
@@ -685,7 +684,7 @@ def octopus_pages_compact(refs, page_map, moves, workspace, stream=None):
 def octopus_pages_rename(page_map, table, lens=None, stream=None):
     """Entries of table (device int32 [n_rows, max_pages], or one row) below ceil(lens / 64) (lens device int32 [n_rows]; None: all) by page_map."""
     n_rows, max_pages = table.shape if table.dim() == 2 else (1, table.numel())
-    _check_ints((page_map, 1), (table, 1), (lens, n_rows))
+    assert _ints_ok(page_map, 1) and _ints_ok(table, 1) and _ints_ok(lens, n_rows)
     code = load().octopus_pages_rename(page_map.data_ptr(), page_map.numel(), table.data_ptr(), n_rows, max_pages, _ptr(lens),
                                        _stream_ptr(stream))
     _check(code, "octopus_pages_rename")
@@ -711,7 +710,7 @@ def page_pools(tensors, n_pages=None):
 def octopus_pages_copy(pools, moves, max_moves=None, stream=None):
     """Pages of every pool of `pools` (page_pools) by the (from, to) pairs of moves, device int32 [2 + 2 max_moves], of which moves[0] count."""
     most = moves.numel() // 2 - 1 if max_moves is None else int(max_moves)
-    _check_ints((moves, 2 + 2 * max(most, 0)))
+    assert _ints_ok(moves, 2 + 2 * max(most, 0))
     code = load().octopus_pages_copy(pools.array, len(pools.array), pools.n_pages, moves.data_ptr(), most, _stream_ptr(stream))
     _check(code, "octopus_pages_copy")
 
@@ -725,20 +724,26 @@ def octopus_verify_drafts(target, draft, draft_tokens, uniforms, tokens_out, n_a
     (any strides with a contiguous last dimension; draft None: drafts that were not drawn), draft_tokens device int32 [n_seq, n_draft] (None
     with no drafts), uniforms device fp32 [n_seq, n_draft + 1], tokens_out device int32 [n_seq, n_draft + 1], n_accepted and draft_lens
     device int32 [n_seq]."""
+    int32 = _int32 or _int32_type()
     n_seq, rows, vocab = target.shape
     t_seq, t_pos, t_one = target.stride()
-    assert t_one == 1 or vocab == 1
-    assert uniforms.is_contiguous() and uniforms.shape == (n_seq, rows) and _dtype_code(uniforms) == DTYPE_F32
-    assert tokens_out.shape == (n_seq, rows) and (rows == 1 or draft_tokens.shape == (n_seq, rows - 1))
-    _check_ints((draft_tokens, 0), (draft_lens, n_seq), (tokens_out, 1), (n_accepted, n_seq))
-    q_args = (None, 0, 0)
-    if draft is not None and rows > 1:
-        q_seq, q_pos, q_one = draft.stride()
-        assert draft.shape == (n_seq, rows - 1, vocab) and draft.dtype == target.dtype and (q_one == 1 or vocab == 1)
-        q_args = (draft.data_ptr(), q_seq, q_pos)
-    code = load().octopus_verify_drafts(target.data_ptr(), _dtype_code(target), t_seq, t_pos, *q_args, _ptr(draft_tokens), _ptr(draft_lens),
-                                        uniforms.data_ptr(), n_seq, rows - 1, vocab, tokens_out.data_ptr(), n_accepted.data_ptr(),
-                                        workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream))
+    shape = (n_seq, rows)
+    assert (t_one == 1 or vocab == 1) and uniforms.is_contiguous() and uniforms.shape == shape and _dtype_code(uniforms) == DTYPE_F32
+    assert tokens_out.dtype is int32 and tokens_out.is_contiguous() and tokens_out.shape == shape
+    assert n_accepted.dtype is int32 and n_accepted.is_contiguous() and n_accepted.numel() >= n_seq
+    assert draft_lens is None or (draft_lens.dtype is int32 and draft_lens.is_contiguous() and draft_lens.numel() >= n_seq)
+    x = q = None
+    q_seq = q_pos = 0
+    if rows > 1:
+        assert draft_tokens.dtype is int32 and draft_tokens.is_contiguous() and draft_tokens.shape == (n_seq, rows - 1)
+        x = draft_tokens.data_ptr()
+        if draft is not None:
+            q_seq, q_pos, q_one = draft.stride()
+            assert draft.shape == (n_seq, rows - 1, vocab) and draft.dtype is target.dtype and (q_one == 1 or vocab == 1)
+            q = draft.data_ptr()
+    code = load().octopus_verify_drafts(target.data_ptr(), _dtype_code(target), t_seq, t_pos, q, q_seq, q_pos, x,
+                                        None if draft_lens is None else draft_lens.data_ptr(), uniforms.data_ptr(), n_seq, rows - 1, vocab,
+                                        tokens_out.data_ptr(), n_accepted.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream))
     _check(code, "octopus_verify_drafts")
 
 

@@ -175,6 +175,25 @@ def test_a_prompt_at_once_and_token_by_token():
     assert torch.equal(x.k_pool, k) and torch.equal(x.v_pool, v)
 
 
+@pytest.mark.parametrize("n_new", [1, 130])
+def test_queries_in_place(n_new):
+    x = Axes(128, 3, 2, 2, 4, n_new, [0, 7])
+    x.append_axes()
+    q = x.q_dev.contiguous()
+    x.append_axes(q=q, q_out=q)
+    assert torch.equal(q, x.q_out)
+
+
+@pytest.mark.parametrize("n_new", [1, 70])
+def test_positions_far_apart(n_new):
+    """Axes 2^30 numbers apart, sequences 2^29: offsets past 32 bits, in elements and in bytes."""
+    far = torch.empty(2 ** 31 + 2 ** 29 + 1000, dtype=torch.int32, device=DEV)
+    x = Axes(64, 3, 2, 1, 2, n_new, [0, 30])
+    pos = far.as_strided((2, n_new, 3), (2 ** 29, 1, 2 ** 30))
+    pos.copy_(x.pos_dev)
+    x.compare(pos=pos)
+
+
 def test_another_stream():
     x = Axes(128, 3, 2, 2, 2, 300, [7, 0])
     side = torch.cuda.Stream()

@@ -229,6 +229,61 @@ def test_compaction(n_pages, used):
     assert not x.model.moves
 
 
+def test_compaction_of_the_largest_pool():
+    """2^24 pages, a third of them in use: the pairs, the counts and the map as the definition has them."""
+    n_pages = 1 << 24
+    used = torch.rand(n_pages, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV) < 0.33
+    ids = torch.arange(n_pages, dtype=torch.int32, device=DEV)
+    refs = torch.where(used, ids % 5 + 1, 0).int()
+    before = refs.clone()
+    page_map, moves = torch.zeros_like(refs), torch.zeros(2 + n_pages, dtype=torch.int32, device=DEV)
+    ws = torch.empty(binding.octopus_pages_workspace(n_pages, 1, 1), dtype=torch.uint8, device=DEV)
+    binding.octopus_pages_compact(refs, page_map, moves, ws)
+    n = int(used.sum())
+    high, low = ids[n:][used[n:]].flip(0), ids[:n][~used[:n]]
+    assert moves[:2].tolist() == [len(high), n] and len(high) == len(low) > 1000000
+    assert torch.equal(moves[2:2 + 2 * len(high)].view(-1, 2), torch.stack([high, low], dim=1))
+    want_map, want_refs = ids.clone(), before.clone()
+    want_map[high.long()] = low
+    want_refs[low.long()], want_refs[high.long()] = before[high.long()], 0
+    assert torch.equal(page_map, want_map) and torch.equal(refs, want_refs)
+
+
+def test_free_pages_at_the_end_of_the_largest_pool():
+    n_pages = 1 << 24
+    refs = torch.ones(n_pages, dtype=torch.int32, device=DEV)
+    refs[[0, 5, n_pages - 3, n_pages - 1]] = 0
+    refs[5] = -7
+    table, lens = torch.zeros((2, 4), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    moves = torch.zeros(6, dtype=torch.int32, device=DEV)
+    ws = torch.empty(binding.octopus_pages_workspace(n_pages, 2, 4), dtype=torch.uint8, device=DEV)
+    binding.octopus_pages_update(refs, table, lens, ints([1, 200]), moves, ws)
+    assert moves[:2].tolist() == [0, 1] and lens.tolist() == [0, 0] and int((refs == 1).sum()) == n_pages - 4
+    binding.octopus_pages_update(refs, table, lens, ints([1, 190]), moves, ws)
+    assert moves[:2].tolist() == [0, 0] and table.tolist() == [[0, 0, 0, 0], [5, n_pages - 3, n_pages - 1, 0]] and bool((refs == 1).all())
+
+
+def test_the_largest_table():
+    """32 rows of 2^25 - 1 entries (4 GiB): forks and growth in the last rows; slots that ask for 2^31 tokens each are told how many pages are missing."""
+    n_seq, per, n_pages = 32, (2 ** 31 - 1) // 64, 64
+    table = torch.zeros((n_seq, per), dtype=torch.int32, device=DEV)
+    ws = torch.empty(binding.octopus_pages_workspace(n_pages, n_seq, per), dtype=torch.uint8, device=DEV)
+    refs, lens = torch.zeros(n_pages, dtype=torch.int32, device=DEV), torch.zeros(n_seq, dtype=torch.int32, device=DEV)
+    moves = torch.zeros(2 + 2 * n_seq, dtype=torch.int32, device=DEV)
+    source = torch.arange(n_seq, dtype=torch.int32, device=DEV)
+    new = torch.zeros_like(lens)
+    new[31] = 200
+    binding.octopus_pages_update(refs, table, lens, new, moves, ws)
+    assert table[31, :4].tolist() == [0, 1, 2, 3]
+    source[29], new[29] = 31, 201
+    new[31] = 201
+    binding.octopus_pages_update(refs, table, lens, new, moves, ws, source=source)
+    assert table[29, :4].tolist() == [0, 1, 2, 4] and moves[:4].tolist() == [1, 0, 3, 4] and refs[:5].tolist() == [2, 2, 2, 1, 1]
+    new.fill_(2 ** 31 - 1)
+    binding.octopus_pages_update(refs, table, lens, new, moves, ws)
+    assert moves[:2].tolist() == [0, n_seq * per - 8 - (n_pages - 5)] and lens.tolist() == [0] * 29 + [201, 0, 201]
+
+
 @pytest.mark.parametrize("bytes_of", [(16,), (16, 32, 48, 16400), (1 << 14, 1 << 17), tuple(16 * (1 + i % 9) for i in range(150))])
 def test_copies_of_every_size_and_number_of_pools(bytes_of):
     rng = np.random.default_rng(len(bytes_of))

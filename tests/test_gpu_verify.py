@@ -71,7 +71,8 @@ class Batch:
         return count
 
 
-@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025, 4097, 32000, 50257, 128256, 300001])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025, 4097, 32000, 50257, 65536, 65537, 128256, 262143, 262144,
+                                   300001])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("sampled", [True, False])
 def test_vocabularies(vocab, dtype, sampled):
@@ -87,6 +88,17 @@ def test_numbers_of_drafts(n_seq, n_draft, sampled, agree):
     count = x.check()
     if agree == 1.0 and sampled:
         assert np.array_equal(count, np.full(n_seq, n_draft) if x.lens is None else x.lens)
+
+
+@pytest.mark.parametrize("sampled", [True, False])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_many_drafts_of_long_rows(sampled, dtype):
+    """Rows of two launches: padded batches, drafts past the 64 that a wavefront looks at."""
+    Batch(20, 5, 66000, dtype, sampled, ragged=True, agree=0.9, seed=21).check()
+    x = Batch(1, 70, 66000, dtype, True, agree=1.0, seed=22)
+    x.draft = x.draft if sampled else None
+    x.target[0, 66, x.x[0, 66]] = 0.0
+    assert x.check().tolist() == [66] or not sampled
 
 
 @pytest.mark.parametrize("where", [0, 1, 62, 63, 64, 127, 128, 199])
@@ -117,7 +129,7 @@ def test_borders_exactly(sampled):
     assert count == [0] * (n - 1) + [1] or not sampled
 
 
-@pytest.mark.parametrize("vocab", [5, 1024, 5000])
+@pytest.mark.parametrize("vocab", [5, 1024, 5000, 70000])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_random_numbers_at_their_ends(vocab, dtype):
     """0, the largest below 1, and what is none: 1, above, below, infinities, NaN; a token without weight is never drawn."""
@@ -133,8 +145,9 @@ def test_random_numbers_at_their_ends(vocab, dtype):
     assert np.all(x.target.float().numpy()[np.arange(len(u)), accepted, last] > 0)
 
 
-def test_numbers_that_are_no_probabilities_count_as_zero():
-    x = Batch(64, 2, 700, seed=5)
+@pytest.mark.parametrize("n_seq,vocab", [(64, 700), (4, 66001)])
+def test_numbers_that_are_no_probabilities_count_as_zero(n_seq, vocab):
+    x = Batch(n_seq, 2, vocab, seed=5)
     rng = np.random.default_rng(0)
     for t in (x.target, x.draft):
         at = torch.from_numpy(rng.random(t.shape) < 0.3)
@@ -143,12 +156,13 @@ def test_numbers_that_are_no_probabilities_count_as_zero():
 
 
 @pytest.mark.parametrize("sampled", [True, False])
-def test_rows_with_nothing_left(sampled):
+@pytest.mark.parametrize("vocab", [2000, 80000])
+def test_rows_with_nothing_left(sampled, vocab):
     """A draft that falls though the target is nowhere above the drafter: the token is the target's; an empty row has none."""
-    x = Batch(6, 1, 2000, sampled=sampled, seed=6)
+    x = Batch(6, 1, vocab, sampled=sampled, seed=6)
     x.target[:, 0] = 0.0
     x.target[0, 0, 77] = 0.25
-    x.target[1, 0, 5], x.target[1, 0, 1999] = 0.25, 0.25
+    x.target[1, 0, 5], x.target[1, 0, vocab - 1] = 0.25, 0.25
     if sampled:
         x.draft[:] = 0.25
         x.x[:2] = [[3], [3]]
@@ -158,7 +172,7 @@ def test_rows_with_nothing_left(sampled):
     x.u[1, 1] = 0.75
     x.check()
     tokens, accepted = x.call()
-    assert tokens[0, 0] == 77 and tokens[1, 0] == 1999 and accepted.tolist() == [0] * 6 and np.all(tokens[2:] == -1)
+    assert tokens[0, 0] == 77 and tokens[1, 0] == vocab - 1 and accepted.tolist() == [0] * 6 and np.all(tokens[2:] == -1)
 
 
 def test_drafts_outside_the_vocabulary_and_counts_out_of_range():
@@ -236,8 +250,9 @@ def test_tokens_come_out_as_the_targets():
         assert 0 < int(accepted.sum()) < n
 
 
-def test_another_stream_and_a_captured_call():
-    x, y = Batch(4, 3, 5000, seed=12), Batch(4, 3, 5000, seed=13)
+@pytest.mark.parametrize("vocab", [5000, 66000])
+def test_another_stream_and_a_captured_call(vocab):
+    x, y = Batch(4, 3, vocab, seed=12), Batch(4, 3, vocab, seed=13)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
     want = [b.expected() for b in (x, y)]
@@ -245,7 +260,7 @@ def test_another_stream_and_a_captured_call():
     assert np.array_equal(got[0], want[0][0])
     target, draft, drafts, u = (x.dev(t).clone() for t in (x.target, x.draft, x.x, x.u))
     tokens, accepted = torch.zeros((4, 4), dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
-    ws = torch.zeros(binding.octopus_verify_workspace(4, 3, 5000), dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(binding.octopus_verify_workspace(4, 3, vocab), dtype=torch.uint8, device=DEV)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         binding.octopus_verify_drafts(target, draft, drafts, u, tokens, accepted, ws)
