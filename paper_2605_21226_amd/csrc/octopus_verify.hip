@@ -77,6 +77,9 @@ __device__ __forceinline__ Row<BF16> draft_row(const VerifyCall &c, int s, int i
 struct Drafts {
     int n, a, fell;
 };
+__device__ __forceinline__ int draft_count(const VerifyCall &c, int s) {
+    return c.draft_lens != nullptr ? min(max(c.draft_lens[s], 0), c.n_draft) : c.n_draft;
+}
 template <bool BF16>
 __device__ __forceinline__ Drafts standing(const VerifyCall &c, int s) {
     const int lane = threadIdx.x % kLanes;
@@ -89,7 +92,7 @@ __device__ __forceinline__ Drafts standing(const VerifyCall &c, int s) {
             x = c.tokens[static_cast<int64_t>(s) * c.n_draft + i];
             u = c.uniforms[static_cast<int64_t>(s) * (c.n_draft + 1) + i];
         }
-        if (i0 == 0) d.n = c.draft_lens != nullptr ? min(max(c.draft_lens[s], 0), c.n_draft) : c.n_draft;
+        if (i0 == 0) d.n = draft_count(c, s);
         const bool is = i < d.n && x >= 0 && x < c.vocab;
         const float p = is ? target_row<BF16>(c, s, i)[x] : 0.0f;
         const float q = c.draft == nullptr ? 1.0f : (is ? draft_row<BF16>(c, s, i)[x] : 0.0f);
@@ -295,6 +298,7 @@ __global__ __launch_bounds__(kLanes) void verify_sums_kernel(VerifyCall c) {
         const double whole = wave_scan(sum.whole), rest = wave_scan(sum.rest);
         if (threadIdx.x == kLanes - 1) c.sums[static_cast<int64_t>(s) * c.pieces + blockIdx.x] = RowSums{whole, rest};
     });
+    if (blockIdx.x == 0 && threadIdx.x == 0) c.accepted[s] = d.a;
 }
 
 // ... and one for the token.
@@ -302,7 +306,8 @@ template <bool BF16>
 __global__ __launch_bounds__(kLanes) void verify_pick_kernel(VerifyCall c) {
     const int s = blockIdx.x;
     const float u = last_uniform(c, s);
-    const Drafts d = standing<BF16>(c, s);
+    Drafts d{draft_count(c, s), c.accepted[s], -1};
+    if (c.draft == nullptr && d.a < d.n) d.fell = c.tokens[static_cast<int64_t>(s) * c.n_draft + d.a];
     with_weights<BF16>(c, s, d, [&](const auto &w) {
         const Found f = find_piece(c.sums + static_cast<int64_t>(s) * c.pieces, c.pieces, u);
         const int first = f.piece * c.piece;
