@@ -39,8 +39,9 @@ __device__ __forceinline__ Slot slot_of(const PagesCall &c, int s) {
 
 // Rows that come from another slot: what they keep is set aside (the row that it comes from may change too), and the counts follow.  A
 // thread has one entry of kShareSlots slots, whose reads are on their way at once; slots of one source that follow each other add to a page's
-// count together (64 samples of a prompt of 1024 pages: 27.3 us with an atomic addition a slot, 8.4 so).
-constexpr int kRowThreads = 256, kShareSlots = 16;
+// count together (64 samples of a prompt of 1024 pages: this launch took 27 us with an atomic addition a slot; the whole call takes 14.1, with
+// 16 slots a thread 18.6).
+constexpr int kRowThreads = 256, kShareSlots = 4;
 __global__ __launch_bounds__(kRowThreads) void pages_share_kernel(PagesCall c) {
     __shared__ Slot slots[kShareSlots];
     const int s0 = blockIdx.y * kShareSlots, j = blockIdx.x * kRowThreads + threadIdx.x;
