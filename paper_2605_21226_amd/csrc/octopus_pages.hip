@@ -474,7 +474,8 @@ __global__ __launch_bounds__(kRowThreads) void pages_rename_kernel(PagesCall c) 
 // does not, since samples of one prompt all read its last page.  Pages at random places, keys and values of eight kv heads at d = 128, 3 bits:
 // 32 pages of eight layers (84 MB read and written) 28 us with ordinary stores, 16.5 with streaming ones, 63 copies of one page of sixteen 50 and 37,
 // 141 pages of eight layers (370 MB) 93 and 82, 4.5 TB/s, where a copy of as much in one piece reaches 5.3; streaming reads too: 21, 57 and 83.
-constexpr int kCopyThreads = 256, kCopyAhead = 4;
+// (256 to 1024 threads and 1024 to 16384 workgroups lie within 5 % of each other; 32 KB a turn was slower.)
+constexpr int kCopyThreads = 512, kCopyAhead = 2;
 constexpr int kPieceWords = kCopyThreads * kCopyAhead;     // of 16 bytes
 __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(CopyCall c) {
     typedef uint32_t word_t __attribute__((ext_vector_type(4)));
@@ -543,7 +544,7 @@ int launch_pages_copy(const CopyCall &c, int32_t n_pools, void *stream) {
         const int64_t n = (c.pools[p].page_bytes / 16 + kPieceWords - 1) / kPieceWords;
         pieces = n > pieces ? n : pieces;
     }
-    const int64_t most = 8192 / n_pools, all = pieces * c.max_moves;
+    const int64_t most = 4096 / n_pools, all = pieces * c.max_moves;
     hipLaunchKernelGGL(pages_copy_kernel, dim3(static_cast<unsigned>(all < most ? all : most), n_pools), dim3(kCopyThreads), 0,
                        static_cast<hipStream_t>(stream), c);
     return static_cast<int>(hipGetLastError());
