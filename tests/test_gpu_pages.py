@@ -35,8 +35,8 @@ class Server:
         self.on_device = [c.to(DEV) for c in self.contents]
         self.pools = binding.page_pools(self.on_device)
 
-    def copy(self):
-        binding.octopus_pages_copy(self.pools, self.moves)
+    def copy(self, stream=None):
+        binding.octopus_pages_copy(self.pools, self.moves, stream=stream)
         for c in self.contents:
             before = c.clone()
             for a, b in self.model.moves:
@@ -59,7 +59,7 @@ class Server:
         self.model.update(new_lens, source, keep_lens)
         binding.octopus_pages_update(self.refs, self.table, self.lens, ints(new_lens), self.moves, self.ws, source=ints(source),
                                      keep_lens=ints(keep_lens), stream=stream)
-        self.copy()
+        self.copy(stream)
         torch.cuda.synchronize()
         self.compare(self.model.missing)
 
@@ -360,3 +360,42 @@ def test_another_stream_and_a_captured_step():
         assert np.array_equal(x.refs.cpu().numpy(), x.model.refs) and np.array_equal(x.table.cpu().numpy(), x.model.table)
         assert all(torch.equal(a, b.cpu()) for a, b in zip(x.contents, x.on_device))
         x.model.check()
+
+
+@pytest.mark.parametrize("n_seq,per", [(9, 5), (64, 200)])
+def test_two_captured_graphs_of_one_workspace(n_seq, per):
+    """Two servers' steps, captured with the same workspace, replayed in turns with eager calls with it in between."""
+    n_pages = n_seq * per * 2
+    pair = [server(n_seq, per, n_pages, [1 + (37 * s + 11 * i) % (TILE * (per - 2)) for s in range(n_seq)], seed=i) for i in range(2)]
+    x, y = pair
+    y.ws = x.ws
+    rng = np.random.default_rng(8)
+    sources = [rng.integers(0, n_seq, size=n_seq) for _ in pair]
+    told = [(ints(s), torch.zeros(n_seq, dtype=torch.int32, device=DEV)) for s in sources]
+    graphs = []
+    torch.cuda.synchronize()
+    for z, (source, new) in zip(pair, told):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            binding.octopus_pages_update(z.refs, z.table, z.lens, new, z.moves, z.ws, source=source)
+            binding.octopus_pages_copy(z.pools, z.moves)
+        graphs.append(graph)
+    for turn in range(6):
+        i = turn % 2
+        z, (source, new) = pair[i], told[i]
+        want = np.minimum(z.model.lens[sources[i]] + rng.integers(-30, 60, size=n_seq), TILE * per)
+        want = np.maximum(want, 0)
+        new.copy_(ints(want))
+        z.moves.fill_(JUNK)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        z.model.update(want, sources[i])
+        for c in z.contents:
+            before = c.clone()
+            for a, b in z.model.moves:
+                c[b] = before[a]
+        z.compare(z.model.missing)
+        other = pair[1 - i]
+        other.update(np.minimum(other.model.lens + 5, TILE * per))      # eager, with the same workspace
+    for z in pair:
+        z.model.check()
