@@ -604,10 +604,12 @@ def octopus_append_paged_axes(cb, k, v, signs, k_pool, v_pool, n_pages, block_ta
     n_pos, pairs, two = rope.shape
     assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
     axis = rope_axis if type(rope_axis) is bytes else bytes(rope_axis)
-    p_seq, p_new, n_axes = rope_pos.shape
-    assert len(axis) == pairs and p_seq == k.shape[0] and p_new == k.shape[1] and rope_pos.dtype is _int32_type()
-    turn = ctypes.byref(RopeAxes(rope.data_ptr(), n_pos, rope_pos.data_ptr(), *rope_pos.stride(), axis, n_axes, 2 * pairs,
+    n_seq, n_new, n_axes = rope_pos.shape
+    assert len(axis) == pairs and rope_pos.dtype is (_int32 or _int32_type())
+    s_seq, s_tok, s_axis = rope_pos.stride()
+    turn = ctypes.byref(RopeAxes(rope.data_ptr(), n_pos, rope_pos.data_ptr(), s_seq, s_tok, s_axis, axis, n_axes, 2 * pairs,
                                  1 if rope_interleaved else 0))
+    assert k.shape[:2] == (n_seq, n_new)
     _append("octopus_append_paged_axes", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
             v_group, stream)
 
@@ -663,11 +665,21 @@ def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, so
     """Slots continue themselves or source[s], keep min(lens, keep_lens, new_lens) tokens and get pages for new_lens: refs device int32
     [n_pages], block_table device int32 [n_seq, max_pages_per_seq], lens, new_lens, source and keep_lens device int32 [n_seq], moves
     device int32 of at least 2 + 2 n_seq, workspace device uint8 of octopus_pages_workspace(...)."""
+    int32 = _int32 or _int32_type()          # (checked in place: a function each cost the call 0.8 us of 6)
     n_seq, max_pages = block_table.shape
-    assert _ints_ok(refs, 1) and _ints_ok(block_table, 1) and _ints_ok(lens, n_seq) and _ints_ok(new_lens, n_seq)
-    assert _ints_ok(source, n_seq) and _ints_ok(keep_lens, n_seq) and _ints_ok(moves, 2 + 2 * n_seq)
-    code = load().octopus_pages_update(refs.data_ptr(), refs.numel(), block_table.data_ptr(), max_pages, lens.data_ptr(), n_seq, _ptr(source),
-                                       _ptr(keep_lens), new_lens.data_ptr(), moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+    assert refs.dtype is int32 and refs.is_contiguous() and block_table.dtype is int32 and block_table.is_contiguous()
+    assert lens.dtype is int32 and lens.is_contiguous() and lens.numel() >= n_seq
+    assert new_lens.dtype is int32 and new_lens.is_contiguous() and new_lens.numel() >= n_seq
+    assert moves.dtype is int32 and moves.is_contiguous() and moves.numel() >= 2 + 2 * n_seq
+    source_at = keep_at = None
+    if source is not None:
+        assert source.dtype is int32 and source.is_contiguous() and source.numel() >= n_seq
+        source_at = source.data_ptr()
+    if keep_lens is not None:
+        assert keep_lens.dtype is int32 and keep_lens.is_contiguous() and keep_lens.numel() >= n_seq
+        keep_at = keep_lens.data_ptr()
+    code = load().octopus_pages_update(refs.data_ptr(), refs.numel(), block_table.data_ptr(), max_pages, lens.data_ptr(), n_seq, source_at,
+                                       keep_at, new_lens.data_ptr(), moves.data_ptr(), workspace.data_ptr(), workspace.nbytes,
                                        _stream_ptr(stream))
     _check(code, "octopus_pages_update")
 

@@ -127,12 +127,12 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
             first_at[i] = INT32_MAX;
         }
     __syncthreads();
-    // whether it holds for any thread, in this round or one before (all threads call it; a barrier)
+    // whether it holds for any thread, in this turn of the loop or one before (all threads call it; a barrier)
     auto any = [&](int which, bool it) {
         if (it) flags[which] = 1;
         __syncthreads();
         const bool is = flags[which] != 0;
-        if constexpr (!ONE) __syncthreads();     // (the next round may set it)
+        if constexpr (!ONE) __syncthreads();     // (the next turn may set it)
         return is;
     };
     SlotPages mine{0, 0, -1, 0};         // ONE: the thread's slot
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kAssignThreads) void pages_assign_kernel(PagesCall 
     int32_t row[kEntries];               // ROWS: what the thread's entries become, -1: nothing new
     const int n_entries = ROWS ? c.n_seq * c.max_pages : 0;
 
-    // f(slot, k, entry, n): the k-th of the slot's `count` items, the n-th of this round; by all threads, whosever they are
+    // f(slot, k, entry, n): the k-th of the slot's `count` items, the n-th of all of them; by all threads, whosever they are
     auto spread = [&](int base, int count, int entry, auto f) {
         int total;
         const int upto = block_scan<kAssignThreads>(count, room[0], &total);
