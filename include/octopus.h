@@ -509,7 +509,8 @@ int octopus_attn_decode_paged_qjl(const octopus_codebooks_t *cb,
  *   k, v         device, element (s, t, h, c) at s*stride_seq + t*stride_tok + h*stride_head + c; both kv_dtype F32/BF16; strides in
  *                elements, multiples of 8, >= 0; bases 16-byte aligned.
  *   new_lens     device int32 [n_seq] or NULL (all n_new): the tokens of each sequence that count (clamped to 0 .. n_new); a padded
- *                batch's others are not looked at, their slots and their rows of q_out stay as they were.
+ *                batch's others are not looked at, their slots and their rows of q_out stay as they were.  Every token that counts is
+ *                written to the page that the table names, whoever else holds it: see octopus_pages_update for what bounds them.
  *   rope         host, or NULL: no rotation.  At position p channels a, b of pair i < dim / 2 become a cos - b sin, a sin + b cos with
  *                (cos, sin) = table[p][i]; pairs are channels i and i + dim / 2, or (interleaved) 2 i and 2 i + 1; channels from dim on
  *                stay.  table: device fp32 [n_pos][dim / 2][2], 16-byte aligned; dim: a multiple of 16, <= head_dim; pos: device
@@ -667,6 +668,12 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb,
  *   Free pages are handed out lowest number first, to the slots in order; a slot's copied page comes first.
  *   If there are fewer than are needed, no slot grows: every lens[s] is the tokens kept, no page is to be copied, and moves[1] says how
  *   many are missing.
+ *   What is appended next has to end at lens: a slot that did not grow (pages ran out, it ended, no more was asked for) has no page of its own
+ *   for another token; the page in which its tokens end may be shared, and entries behind that name pages of other slots.  So a step
+ *   that does not read moves[1] on the host gives octopus_append_paged (_axes) start_pos = the tokens kept and
+ *       new_lens[s] = min(max(lens[s] - start_pos[s], 0), n_new),
+ *   made on the device from the lens that this call left, and the attention the same numbers as q_lens.  (octopus_encode_paged and its kin have no
+ *   new_lens: they are for steps known to have grown.)
  *     source, keep_lens, new_lens   device int32 [n_seq] (the first two may be NULL); token counts are clamped to what a row holds, page ids to the pool.
  *     moves      device int32 [2 + 2 n_seq]: [0] pages to be copied, [1] pages missing, then (from, to) pairs in the order of slots.  Give it
  *                to octopus_pages_copy before anything is appended; no page is both a from and a to.

@@ -664,7 +664,8 @@ def _ints_ok(t, least):
 def octopus_pages_update(refs, block_table, lens, new_lens, moves, workspace, source=None, keep_lens=None, stream=None):
     """Slots continue themselves or source[s], keep min(lens, keep_lens, new_lens) tokens and get pages for new_lens: refs device int32
     [n_pages], block_table device int32 [n_seq, max_pages_per_seq], lens, new_lens, source and keep_lens device int32 [n_seq], moves
-    device int32 of at least 2 + 2 n_seq, workspace device uint8 of octopus_pages_workspace(...)."""
+    device int32 of at least 2 + 2 n_seq, workspace device uint8 of octopus_pages_workspace(...).  A slot may be left without pages for
+    new_lens (moves[1]): what is appended goes with new_lens=(lens - start_pos).clamp(0, n_new)."""
     int32 = _int32 or _int32_type()          # (checked in place: a function each cost the call 0.8 us of 6)
     n_seq, max_pages = block_table.shape
     assert refs.dtype is int32 and refs.is_contiguous() and block_table.dtype is int32 and block_table.is_contiguous()
