@@ -707,23 +707,25 @@ class PagePools:
     """The pools that octopus_pages_copy copies pages of; made once, by page_pools, and kept with the pools."""
 
     def __init__(self, tensors, n_pages):
-        self.tensors, self.n_pages = tensors, n_pages
+        self.tensors, self.n_pages, self.device = tensors, n_pages, tensors[0].device
         self.array = (Pool * len(tensors))(*[Pool(t.data_ptr(), t.nbytes // n_pages) for t in tensors])
 
 
 def page_pools(tensors, n_pages=None):
-    """tensors: device, contiguous, each n_pages pages (None: the first dimension of each)."""
+    """tensors: of one device, contiguous, each n_pages pages (None: the first dimension of each)."""
     tensors = list(tensors)
     n_pages = tensors[0].shape[0] if n_pages is None else int(n_pages)
+    assert all(t.device == tensors[0].device for t in tensors)
     assert n_pages >= 1 and all(t.is_contiguous() and t.nbytes % n_pages == 0 for t in tensors)
     assert all(t.dim() == 1 or t.shape[0] == n_pages for t in tensors)
     return PagePools(tensors, n_pages)
 
 
 def octopus_pages_copy(pools, moves, max_moves=None, stream=None):
-    """Pages of every pool of `pools` (page_pools) by the (from, to) pairs of moves, device int32 [2 + 2 max_moves], of which moves[0] count."""
+    """Pages of every pool of `pools` (page_pools) by the (from, to) pairs of moves, int32 [2 + 2 max_moves] on the pools' device, of which
+    moves[0] count."""
     most = moves.numel() // 2 - 1 if max_moves is None else int(max_moves)
-    assert _ints_ok(moves, 2 + 2 * max(most, 0))
+    assert _ints_ok(moves, 2 + 2 * max(most, 0)) and moves.device == pools.device
     code = load().octopus_pages_copy(pools.array, len(pools.array), pools.n_pages, moves.data_ptr(), most, _stream_ptr(stream))
     _check(code, "octopus_pages_copy")
 
