@@ -187,8 +187,10 @@ struct ManyAxes {
 
 // Few tokens (a decode step appends one per sequence): a wavefront per (token, KV head), which takes the key, the value and the
 // head's queries as rows side by side, eight channels a lane, and encodes the key a triplet per lane.
+// (the call by value: by reference the compiler copies loads of the rows' loop, 236 bytes and two registers more at d = 128, and a single
+// token takes 5.36 us instead of 5.22)
 template <class P, class Turn>
-__device__ __forceinline__ void append_token(const AppendCall &a, const Turn &turn) {
+__device__ __forceinline__ void append_token(const AppendCall a, const Turn &turn) {
     constexpr int D = P::D, LPR = D / 8, ROWS = kWave / LPR;
     constexpr int NX = P::BD0 > 2 || P::BD1 > 2 ? 1 << (P::BD0 > P::BD1 ? P::BD0 : P::BD1) : 4;
     constexpr int NR = 1 << (P::BN0 > P::BN1 ? P::BN0 : P::BN1);
