@@ -583,18 +583,37 @@ _NO_QUERIES = (None, 0, 0, 0, 0, 0, None, 0)
 
 
 def octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos=None, new_lens=None, rope=None,
-                         rope_interleaved=False, rope_pos=None, q=None, q_out=None, v_bits=0, v_group=0, stream=None):
+                         rope_interleaved=False, rope_pos=None, q=None, q_out=None, v_bits=0, v_group=0, stream=None, _axes=None):
     """A step's new tokens into pages: k and v device [n_seq, n_new, n_kv_heads, d] and q [n_seq, n_new, n_q_heads, d] (any strides with
     contiguous channels; k and v of one type), rope device fp32 [n_pos, dim / 2, 2] contiguous (cos, sin) or None, rope_pos device
     int32 [n_seq] or None (the slots), q_out device [n_seq, n_new, n_q_heads, d] contiguous, v_pool device bf16 pages or, with v_bits,
     uint8 rows; start_pos and new_lens device int32 [n_seq] or None."""
-    turn = None
+    # (_axes: the rotation of octopus_append_paged_axes, whose body this is.  A function of its own for what the two share cost this call 0.25 us of 7)
+    n_seq, n_new, n_kv, d = shape = k.shape
+    _check_pools(cb.plan, d, k_pool, v_pool, n_pages, n_kv, v_bits, v_group)
+    ks, kt, kh, kc = k.stride()
+    vs, vt, vh, vc = v.stride()
+    b_seq, max_pages = block_table.shape
+    assert kc == 1 and vc == 1 and v.shape == shape and v.dtype == k.dtype and block_table.is_contiguous() and b_seq == n_seq
+    turn = _axes
     if rope is not None:
         n_pos, pairs, two = rope.shape
         assert two == 2 and rope.is_contiguous() and _dtype_code(rope) == DTYPE_F32
         turn = ctypes.byref(Rope(rope.data_ptr(), n_pos, _ptr(rope_pos), 2 * pairs, 1 if rope_interleaved else 0))
-    _append("octopus_append_paged", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
-            v_group, stream)
+    if q is not None:
+        qs, qt, qh, qc = q.stride()
+        q_seq, q_new, n_qh, q_d = q_shape = q.shape
+        assert qc == 1 and q_seq == n_seq and q_new == n_new and q_d == d and q_out.is_contiguous() and q_out.shape == q_shape
+        q_args = (q.data_ptr(), _dtype_code(q), qs, qt, qh, n_qh, q_out.data_ptr(), _dtype_code(q_out))
+    else:
+        q_args = _NO_QUERIES
+    lib = load()
+    code = (lib.octopus_append_paged if _axes is None else lib.octopus_append_paged_axes)(
+        ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, _dtype_code(k), n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
+        _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), max_pages, _ptr(start_pos),
+        _stream_ptr(stream))
+    if code:
+        _check(code, "octopus_append_paged" if _axes is None else "octopus_append_paged_axes")
 
 
 def octopus_append_paged_axes(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, rope, rope_axis, rope_pos, start_pos=None,
@@ -610,29 +629,8 @@ def octopus_append_paged_axes(cb, k, v, signs, k_pool, v_pool, n_pages, block_ta
     turn = ctypes.byref(RopeAxes(rope.data_ptr(), n_pos, rope_pos.data_ptr(), s_seq, s_tok, s_axis, axis, n_axes, 2 * pairs,
                                  1 if rope_interleaved else 0))
     assert k.shape[:2] == (n_seq, n_new)
-    _append("octopus_append_paged_axes", cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits,
-            v_group, stream)
-
-
-def _append(name, cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, turn, q, q_out, v_bits, v_group, stream):
-    n_seq, n_new, n_kv, d = shape = k.shape
-    _check_pools(cb.plan, d, k_pool, v_pool, n_pages, n_kv, v_bits, v_group)
-    ks, kt, kh, kc = k.stride()
-    vs, vt, vh, vc = v.stride()
-    b_seq, max_pages = block_table.shape
-    assert kc == 1 and vc == 1 and v.shape == shape and v.dtype == k.dtype and block_table.is_contiguous() and b_seq == n_seq
-    if q is not None:
-        qs, qt, qh, qc = q.stride()
-        q_seq, q_new, n_qh, q_d = q_shape = q.shape
-        assert qc == 1 and q_seq == n_seq and q_new == n_new and q_d == d and q_out.is_contiguous() and q_out.shape == q_shape
-        q_args = (q.data_ptr(), _dtype_code(q), qs, qt, qh, n_qh, q_out.data_ptr(), _dtype_code(q_out))
-    else:
-        q_args = _NO_QUERIES
-    code = getattr(load(), name)(
-        ctypes.byref(cb), k.data_ptr(), ks, kt, kh, v.data_ptr(), vs, vt, vh, _dtype_code(k), n_seq, n_kv, n_new, _ptr(new_lens), turn, *q_args,
-        _ptr(signs), _ptr(k_pool), _ptr(v_pool), v_bits, v_group, n_pages, block_table.data_ptr(), max_pages, _ptr(start_pos),
-        _stream_ptr(stream))
-    _check(code, name)
+    octopus_append_paged(cb, k, v, signs, k_pool, v_pool, n_pages, block_table, start_pos, new_lens, q=q, q_out=q_out, v_bits=v_bits, v_group=v_group,
+                         stream=stream, _axes=turn)
 
 
 def octopus_read_paged(cb, signs, k_pool, v_pool, n_pages, block_table, k_out, v_out, start_pos=None, lens=None, v_bits=0, v_group=0,
