@@ -685,7 +685,7 @@ int octopus_attn_decode_paged_prefix(const octopus_codebooks_t *cb,
  *   to the next, until they are 0 .. n - 1.
  *     page_map   device int32 [n_pages]: a page's new number (its own where it stays).
  *     moves      device int32 [2 + 2 (n_pages / 2)]: [0] pages to be copied, [1] n, then (from, to) pairs, highest page first.
- *   refs follow.  Every table has to follow by octopus_pages_rename, and every pool by octopus_pages_copy.  One launch up to 65536 pages,
+ *   refs follow.  Every table has to follow by octopus_pages_rename, and every pool by octopus_pages_copy.  One launch up to 16384 pages,
  *   else three.
  * octopus_pages_rename: entries below ceil(lens[r] / 64) of each row r (lens NULL: all) become page_map[entry]; a block table, or
  *   (n_rows 1, prefix_len) a prefix_table.

@@ -402,28 +402,19 @@ __device__ __forceinline__ void apply_move(const PagesCall &c, int i) {
     c.page_map[from] = to;
 }
 
-// Pools of up to 65536 pages: one workgroup (three launches of the form below took 8.3 us for 1100 pages, this one 6.1).
-constexpr int kCompactRounds = 4;
+// Pools of as many pages as one workgroup's threads look at once, 16384: one launch.  Larger ones: three, whose time hardly grows (us a call in a captured
+// graph, half of the pages in use / nine tenths, one launch and three: 1100 pages 5.2 / 5.1 and 7.2 / 6.9, 8192 7.9 / 6.1 and 8.2 / 7.5, 16384
+// 12.2 / 8.2 and 8.4 / 7.7, 32768 21 / 13 and 8.4 / 8.6, 65536 39 / 23 and 8.7 / 9.0.  An eager caller waits 10 us for three launches longer than
+// for one, and meets them at 20000 pages, a captured step at 9000; the limit lies between).
+constexpr int kCompactPages = kAssignThreads * kPerThread;
 __global__ __launch_bounds__(kAssignThreads) void pages_compact_kernel(PagesCall c) {
     __shared__ int room[kAssignThreads / kScanLanes];
-    const int tid = threadIdx.x;
-    uint32_t used[kCompactRounds];
-    int below[kCompactRounds], n_used = 0;
-#pragma unroll
-    for (int r = 0; r < kCompactRounds; ++r) used[r] = used_pages(c, (r * kAssignThreads + tid) * kPerThread);
-#pragma unroll
-    for (int r = 0; r < kCompactRounds; ++r) {
-        if (r * kAssignThreads * kPerThread >= c.n_pages) break;
-        int total;
-        const int n = static_cast<int>(__popc(used[r]));
-        below[r] = n_used + block_scan<kAssignThreads>(n, room, &total) - n;
-        n_used += total;
-    }
-#pragma unroll
-    for (int r = 0; r < kCompactRounds; ++r) {
-        if (r * kAssignThreads * kPerThread >= c.n_pages) break;
-        pair_pages(c, (r * kAssignThreads + tid) * kPerThread, used[r], below[r], n_used);
-    }
+    const int tid = threadIdx.x, at = tid * kPerThread;
+    const uint32_t used = used_pages(c, at);
+    const int own = static_cast<int>(__popc(used));
+    int n_used;
+    const int below = block_scan<kAssignThreads>(own, room, &n_used) - own;
+    pair_pages(c, at, used, below, n_used);
     __syncthreads();
     const int n = __hip_atomic_load(c.moves, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     for (int i = tid; i < n; i += kAssignThreads) apply_move(c, i);
@@ -522,7 +513,7 @@ int launch_pages_update(const PagesCall &c, void *stream) {
 
 int launch_pages_compact(const PagesCall &c, void *stream) {
     const hipStream_t on = static_cast<hipStream_t>(stream);
-    if (c.n_pages <= kCompactRounds * kAssignThreads * kPerThread) {
+    if (c.n_pages <= kCompactPages) {
         hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kAssignThreads), 0, on, c);
         return static_cast<int>(hipGetLastError());
     }
