@@ -7,9 +7,9 @@
 // key that the encoder takes: what octopus_encode_paged computes of rotated keys, without their rounding to bf16 in between.
 // A token of an image or a video has a position on each of several axes (frame, row, column), and pair i goes by the one that the
 // caller's map gives it: (cos, sin) = table[p_axis(i)][i].  Those kernels (append_*_axes_kernel) differ in nothing else.  A pair's entry is
-// read by itself there, whatever the map, twice as many reads as of one position's row: 15840 patches take 111 us where tokens in a row take
-// 96 (94 if the reads were as wide and no positions had to be read), 64 single tokens 8.0 instead of 7.4.  Wide reads for maps that allow
-// them, beside these by a branch, cost more than they saved (113), by threads too (114).
+// read by itself there, whatever the map, twice as many reads as of one position's row: 15840 patches take 104 to 111 us where tokens in a row
+// take 96 (94 if the reads were as wide and no positions had to be read), 64 single tokens 7.8 instead of 7.4.  Wide reads for maps that allow
+// them, beside these by a branch, cost more than they saved (113 in place of 111), by threads too (114).
 //
 // What bounds it: memory, for long prompts -- queries, keys and values come and go once, the records are a quarter of the keys -- and
 // latency for a few tokens.  Measured at d = 128, 3 bits, 32 query and 8 KV heads, bf16: 15877 tokens, 366 MB, in 97 us, 3.8 TB/s

@@ -402,10 +402,9 @@ __device__ __forceinline__ void apply_move(const PagesCall &c, int i) {
     c.page_map[from] = to;
 }
 
-// Pools of as many pages as one workgroup's threads look at once, 16384: one launch.  Larger ones: three, whose time hardly grows (us a call in a captured
-// graph, half of the pages in use / nine tenths, one launch and three: 1100 pages 5.2 / 5.1 and 7.2 / 6.9, 8192 7.9 / 6.1 and 8.2 / 7.5, 16384
-// 12.2 / 8.2 and 8.4 / 7.7, 32768 21 / 13 and 8.4 / 8.6, 65536 39 / 23 and 8.7 / 9.0.  An eager caller waits 10 us for three launches longer than
-// for one, and meets them at 20000 pages, a captured step at 9000; the limit lies between).
+// Pools of as many pages as one workgroup's threads look at once, 16384: one launch.  Larger ones: three, whose time hardly grows.  us a call in a
+// captured graph, half of the pages in use, one launch / three: 1100 pages 3.6 / 7.2, 16384 10.1 / 8.4; with the workgroup going on in rounds
+// of 16384, 32768 21 / 8.4 and 65536 39 / 8.7 (nine tenths in use 13 / 8.6 and 23 / 9.0).  An eager caller waits 7 us longer for three launches.
 constexpr int kCompactPages = kAssignThreads * kPerThread;
 __global__ __launch_bounds__(kAssignThreads) void pages_compact_kernel(PagesCall c) {
     __shared__ int room[kAssignThreads / kScanLanes];

@@ -4,8 +4,10 @@
 // after them is drawn from the weights r = max(p_a - q_a, 0) if draft a fell (tokens come out distributed as the target's), from p_a
 // if all of them stand: the first token whose running sum of r exceeds u times the whole sum.
 //
-// A call reads a handful of numbers to find a, and then one row of each of the two distributions: memory bounds it for many sequences
-// (256 x 128256 tokens in fp32, 262 MB, 34 us), latency for few (1 x 8000 tokens 5.4 us, four reads that wait for each other).  A row is
+// A call reads a handful of numbers to find a, and then the target's row, and the drafter's where a draft fell.  What bounds it is latency: for few
+// sequences four reads that wait for each other (1 x 8000 tokens 5.5 us), for many the same chain in front of each wavefront's one piece (256 x
+// 128256 tokens in fp32, a third of whose drafts fall, 172 MB, 38 us with other inputs each call, 4.5 TB/s of a plain read's 7.07; 31 us with
+// the same inputs, which the last-level cache holds).  A row is
 // cut into pieces, a wavefront each, that are summed; then a wavefront finds the piece in which the running sum gets there, reads it once
 // more and finds the token.  Differences and sums are 64-bit numbers: u has 24 bits, and a running sum over 10^5 tokens has to tell neighbours
 // apart that differ by less.  Rows that are subtracted from and rows that are not have code of their own, and pieces inside a row need no
@@ -321,9 +323,20 @@ int launch_verify(VerifyCall c, void *stream) {
     const hipStream_t on = static_cast<hipStream_t>(stream);
     c.piece = (c.vocab / (kMostPieces * kRound) + 1) * kRound;
     c.pieces = (c.vocab + c.piece - 1) / c.piece;
-    // Rows of up to 64 pieces in one launch, the others in two (us a call in a captured graph, fp32, one launch / two: 1 sequence x 8000 tokens 5.4 /
-    // 6.9, 1 x 32000 6.8 / 6.7, 64 x 32000 9.6 / 9.5, 512 x 32000 21 / 24, 8 x 50257 9.6 / 7.2, 1 x 64000 8.1 / 6.5, 1 x 128256 13.5 / 6.6,
-    // 64 x 128256 20 / 15, 256 x 128256 39 / 34; a launch costs its caller 4 us).
+    // Rows of up to 64 pieces in one launch, the others in two.  us a call, fp32, one launch / two, of sequences whose drafts all fell (two rows each
+    // are read; of one row each, where all stood or have no probabilities, in brackets):
+    //                    captured                     eager
+    //   1 x 8000         5.5 / 6.7   (4.6 / 5.9)      5.9 / 8.2   (6.1 / 8.9)
+    //   1 x 32000        7.5 / 6.2   (5.8 / 5.7)      7.3 / 9.5   (6.4 / 9.4)
+    //   512 x 32000      28.7 / 30.7 (14.7 / 17.6)    27.9 / 30.4 (14.2 / 17.2)
+    //   8 x 50257        9.3 / 6.9   (7.0 / 6.5)      9.1 / 9.4   (7.0 / 9.4)
+    //   256 x 50257      22.5 / 25.7 (12.2 / 15.2)    22.2 / 25.2 (11.8 / 14.8)
+    //   1 x 64000        10.5 / 6.3  (7.7 / 5.8)      10.4 / 9.2  (7.5 / 9.5)
+    //   64 x 64000       13.2 / 13.0 (9.4 / 9.8)      12.7 / 12.8 (9.1 / 9.8)
+    //   1 x 128256       16.5 / 6.2  (11.4 / 5.7)     16.5 / 9.1  (11.1 / 9.3)
+    //   64 x 128256      24.2 / 17.4 (13.2 / 11.9)    23.6 / 16.9 (12.8 / 11.8)
+    // The limit is where eager calls come out even, whose caller needs 3 us for a second launch; many sequences gain by it in graphs as well, and a
+    // captured call of a few sequences pays for it, at most 4.2 us (1 x 64000).
     if (c.pieces <= 64) {
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(c.n_seq), dim3(kRowWaves * kLanes), 0, on, c); };
         if (c.is_bf16) go(verify_row_kernel<true>);
